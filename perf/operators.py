@@ -171,15 +171,15 @@ def _bytes(n):
 
 def _table(c, g):
     """Pages of the sequences' rows at random places of a pool: the table [B][Hkv][pages], the pool's rows.  An entry
-    past a sequence's rows repeats its first page (page 0 for a sequence without rows)."""
+    past a sequence's rows repeats its first page (one page behind all others for the sequences without rows)."""
     page, Hkv, lens = c["page"], c["Hkv"], _lens(c)
     need = torch.tensor([-(-n // page) for n in lens], device=DEV)
     per = max(1, int(need.max()))
     has = torch.arange(per, device=DEV)[None, None, :] < need[:, None, None].expand(-1, Hkv, 1)
     total = int(need.sum()) * Hkv
-    table = torch.zeros((len(lens), Hkv, per), dtype=torch.int32, device=DEV)
+    table = torch.full((len(lens), Hkv, per), total * page, dtype=torch.int32, device=DEV)
     table[has] = torch.randperm(total, generator=g, device=DEV).to(torch.int32) * page
-    return torch.where(has, table, table[:, :, :1]).contiguous(), max(1, total) * page
+    return torch.where(has, table, table[:, :, :1]).contiguous(), (total + (min(lens) == 0)) * page
 
 
 def _prepare_fetch4(c, g):
