@@ -31,6 +31,11 @@
  *   sg_spec_quota, sg_spec_push, sg_spec_commit
  *                   speculative transfer of the remaining KV blocks in
  *                   importance order (Section 4.3)
+ *   sg_fetch_fp4    sg_fetch into or out of a paged pool of 4-bit rows
+ *   sg_decode_attn_fp4  sg_decode_attn over such a pool, optionally
+ *                   accumulating the attention weight of every row
+ *   sg_decode_attn_acc  sg_decode_attn accumulating the same weights
+ *   sg_evict        cuts paged sets to a budget by accumulated weight
  *
  * Conventions for every call:
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).  Every
@@ -70,6 +75,7 @@ extern "C" {
 typedef enum {
     SG_F32 = 0,
     SG_BF16 = 1,
+    SG_FP4 = 2,   /* 4-bit rows: only the calls that name it take it (see sg_fetch_fp4) */
     /* range markers: a dtype argument may hold any int (others are rejected
        with SG_EINVAL); they give the enum the range of int in C++ too */
     SG_DTYPE_INT_MIN_ = -2147483647 - 1,
@@ -496,6 +502,120 @@ int sg_spec_push(void *stream, sg_dtype dt, int L, int Hkv, int d, int64_t T, in
  */
 int sg_spec_commit(void *stream, int L, int Hkv, int64_t T, int64_t s0, int64_t N, int M, int nblk,
                    const int32_t *ids, int8_t *mask, float *rem);
+
+/* ---------------------------------------------------------------- 4-bit rows
+ * A pool (or source) of SG_FP4 rows is three arrays of `rows` rows:
+ *
+ *   k, v    uint8 [rows][d / 2]: codes, channel 2i in the low nibble of byte i;
+ *   s       uint8 [rows][2][d / 32]: scale bytes of the K row, then of the V
+ *           row, one per 32 channels.
+ *
+ * A code is a sign (bit 3) over one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6 (E2M1); a scale byte e stands for 2^(e - 127), 255 for NaN (E8M0); a value
+ * is code x scale, exact in bf16.  A row of d = 128 is 68 bytes (bf16: 256).
+ *
+ * Storing a block of 32 channels with largest magnitude t: the scale is the
+ * smallest 2^e with t <= 7 x 2^e (byte 2 at least, 252 at most), every channel
+ * goes to the nearest code times the scale (halves to the even code), and
+ * magnitudes above 6 x 2^e to 6 x 2^e.  A block that holds an infinity or NaN
+ * is stored as byte 255 with codes 0 and reads as NaN.
+ *
+ * sg_fetch_fp4: sg_fetch where the source rows, the pool's rows or both are
+ * SG_FP4 (at least one of them): SG_F32 or SG_BF16 rows are rounded to 4 bits
+ * on their way into a 4-bit pool, 4-bit rows are copied into one as they are,
+ * or read back as SG_F32 or SG_BF16 values.  Rows, index, page table and what
+ * is skipped are as for sg_fetch; appending a token is a call with one entry
+ * per row and dst_start = the rows' counts.
+ *
+ *   s_src, s_pool  the scales, device (s_src: or pinned host) memory; required
+ *           with SG_FP4 on that side and NULL otherwise.
+ * All row arrays must be 16-byte aligned; source and pool must not overlap.
+ */
+int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows, const int32_t *row_off,
+                 int64_t total, const int32_t *index, const int32_t *n_valid, const int64_t *src_row_base,
+                 int64_t src_rows, const void *k_src, const void *v_src, const uint8_t *s_src,
+                 const int32_t *page_table, int page_size, int max_pages, const int32_t *dst_start,
+                 void *k_pool, void *v_pool, uint8_t *s_pool, int64_t pool_rows);
+
+/* ---------------------------------------------------------------- accumulated weights
+ * Attention that also adds up how much of it every row of a set receives, the
+ * measure by which sg_evict cuts the set: with p[g][i] the probability of
+ * logical row i under q head g,
+ *
+ *   weight_out[b][h][i] = decay * weight_in[b][h][i] + sum over g of group h of p[g][i]
+ *
+ * for i < n (fp32).  weight_in NULL stands for zeros; weight_out may be
+ * weight_in.  Rows of the arrays are weight_stride floats (at least max_pages *
+ * page_size); entries at and past n are left as they are.  A row outside the
+ * pool receives 0.  0 <= decay <= 1 (1: plain sums).
+ *
+ * sg_decode_attn_acc: sg_decode_attn (same arguments and rules, dt SG_F32 or
+ *   SG_BF16, G in {1, 2, 4, 8, 16}) with the weights, which are required.
+ * sg_decode_attn_fp4: the same attention over a pool of 4-bit rows (k_pool,
+ *   v_pool, s_pool as above), any 1 <= G <= 16; dt is the type of q.  The
+ *   stored values are used exactly and sums are fp32, so out differs from
+ *   attention over the values in fp32 by fp32 rounding only.  weight_out may be
+ *   NULL (then weight_in too): attention alone.
+ * A NaN row makes the outputs and weights of its unit NaN.
+ *   ws      device workspace of at least the matching size, 16-byte aligned
+ *           (logits of every row and split states); no initialisation needed,
+ *           calls that share one must be ordered.  `weights` of the size call:
+ *           whether weight_out is given.
+ */
+size_t sg_decode_attn_acc_workspace_size(int B, int Hq, int Hkv, int d, int max_pages, int page_size);
+int sg_decode_attn_acc(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d, float scale, const void *q,
+                       const void *k_pool, const void *v_pool, int64_t pool_rows, const int32_t *page_table,
+                       const int32_t *n_rows, int page_size, int max_pages, float *out, const float *weight_in,
+                       float decay, float *weight_out, int64_t weight_stride, void *ws, size_t ws_bytes);
+size_t sg_decode_attn_fp4_workspace_size(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int weights);
+int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d, float scale, const void *q,
+                       const uint8_t *k_pool, const uint8_t *v_pool, const uint8_t *s_pool, int64_t pool_rows,
+                       const int32_t *page_table, const int32_t *n_rows, int page_size, int max_pages, float *out,
+                       const float *weight_in, float decay, float *weight_out, int64_t weight_stride, void *ws,
+                       size_t ws_bytes);
+
+/* ---------------------------------------------------------------- sg_evict
+ * Cuts paged sets to a budget by accumulated weight, in place.  Unit u (a
+ * sequence and KV head) holds n = n_rows[u] rows (clamped to [0, max_pages *
+ * page_size]) and keeps n_kept[u] = k = min(budget[u], n) of them:
+ *
+ *   - guarded rows first: those holding a token position below `sinks` or at or
+ *     above recent_from[u] (position = pos[u][i], or i when pos is NULL);
+ *   - then larger weight first;
+ *   - equal weights, and guarded rows among themselves, by lower row; NaN ranks
+ *     below every number.
+ *
+ * The order of a set's rows does not matter to attention (Section 4.2), so
+ * only the holes are filled: the kept rows at and past k, in ascending order,
+ * move to the rows below k that are not kept, in ascending order.  K row, V row
+ * and (SG_FP4) scales, weight and position move together.  Afterwards rows
+ * [0, k) hold the kept ones, weight_out[u][k .. n) is 0 and pos_out[u][k .. n)
+ * is -1; entries at and past n are left as they are, and the pages past row k
+ * are the caller's to reuse.
+ *
+ *   dt      SG_F32, SG_BF16 or SG_FP4 (k_pool, v_pool: codes; s_pool: scales,
+ *           NULL for the other types); d 64 or 128.
+ *   page_table device int32 [units][max_pages] as for sg_decode_attn.  The pages
+ *           of all units must be distinct (a shared page would be moved under
+ *           its other owner).  A move from or to a row outside [0, pool_rows)
+ *           copies no K/V row.
+ *   budget  device int32 [units] (below 0 counts as 0).
+ *   weight, pos  device [units][stride], stride >= max_pages * page_size floats
+ *           or int32; pos may be NULL, then pos_out must be NULL.
+ *   n_kept, weight_out, pos_out  as n_rows, weight, pos; each may be its input
+ *           (in place) and must not otherwise overlap it.  With outputs of
+ *           their own, the same call made again writes the same results.
+ *   sinks >= 0 (0: none); recent_from device int32 [units] or NULL (none).
+ *   ws      device workspace of at least sg_evict_workspace_size(...) bytes,
+ *           16-byte aligned.
+ * Requirements: max_pages * page_size <= 81920.
+ */
+size_t sg_evict_workspace_size(int units, int max_pages, int page_size);
+int sg_evict(void *stream, sg_dtype dt, int units, int d, void *k_pool, void *v_pool, uint8_t *s_pool,
+             int64_t pool_rows, const int32_t *page_table, const int32_t *n_rows, int page_size, int max_pages,
+             const int32_t *budget, const float *weight, const int32_t *pos, int64_t stride, int sinks,
+             const int32_t *recent_from, int32_t *n_kept, float *weight_out, int32_t *pos_out, void *ws,
+             size_t ws_bytes);
 
 #ifdef __cplusplus
 }

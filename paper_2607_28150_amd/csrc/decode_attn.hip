@@ -42,8 +42,13 @@
 // directly; otherwise the split's state goes to the workspace and a merge
 // kernel combines the splits in a fixed order.  All reductions have a fixed
 // order, so results are deterministic.
+//
+// sg_decode_attn_acc is the same kernel with one store more per step, each
+// row's logits into the workspace, and a second launch that joins the splits
+// and turns the logits into weights (decode_weights.h) in the place of the merge.
 #include <mutex>
 
+#include "decode_weights.h"
 #include "sg_internal.h"
 
 namespace sg {
@@ -152,12 +157,15 @@ __device__ __forceinline__ float row_groups_sum(float x) {
 
 // Grid: x = (sequence, KV head) unit, y = split of the unit's rows, z = group
 // of HG q heads within the KV head's G.  See the top of the file.
-template <typename T, int D, int HG>
+// ACC: the logits of every row go to z_out [unit][G][z_stride] and the state of
+// every split, a single one too, to the workspace.
+template <typename T, int D, int HG, bool ACC>
 __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_kernel(
     int Hq, int Hkv, float scale_log2, const T *__restrict__ q, const v4u *__restrict__ k_pool,
     const v4u *__restrict__ v_pool, int64_t pool_rows, const int32_t *__restrict__ page_table,
     const int32_t *__restrict__ n_rows, int page_size, uint32_t page_mul, int page_shift, int max_pages,
-    int64_t split_rows, float *__restrict__ out, float *__restrict__ ws, int nunits, int parts) {
+    int64_t split_rows, float *__restrict__ out, float *__restrict__ ws, int nunits, int parts,
+    float *__restrict__ z_out, int64_t z_stride) {
     using S = DecodeShape<T, D, HG>;
     constexpr int PER16 = Elem<T>::PER16;  // elements per 16-byte vector
     constexpr int LPR = S::LPR, VPL = S::VPL, RPS = S::RPS, WAVES = S::WAVES, NS = S::NS;
@@ -378,6 +386,26 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         }
         return __any(grow);
     };
+    // the logits of row lr (this lane's) for the weights: lane c < HG of the row
+    // stores head c's.  The wait for the ring's loads counts loads alone, so a
+    // store in flight only makes it wait for more of them than it needs.
+    auto keep_logits = [&](int64_t lr, const float (&z)[HG]) {
+        if constexpr (ACC) {
+            const int gl0 = (int)blockIdx.z * HG;      // first head within the KV group
+            float x = z_lane;
+            int head = hd;
+            bool mine = (lane & 1) == 0;
+            if constexpr (!TRANS) {
+                static_assert(HG <= LPR, "a lane per head");
+                head = c;
+                mine = c < HG;
+                x = z[0];
+#pragma unroll
+                for (int g = 1; g < HG; ++g) x = c == g ? z[g] : x;
+            }
+            if (mine && lr < w1) z_out[(unit * G + gl0 + head) * z_stride + lr] = x;
+        }
+    };
     // p = 2^(z - m) into l and, weighted over the lane's V slices, into o
     auto accumulate = [&](const char *sb, const float (&z)[HG]) {
         v4u vv[VPL];
@@ -475,7 +503,9 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
                 issue(w0 + (int64_t)(i + NS - 1) * RPS, (i + NS - 1) % NS, valid);
                 wait_vmem<(NS - 1) * 2 * VPL>();          // step i has landed
                 const char *sb = myring + (i % NS) * SLOTB;
-                if (logits(sb, (valid >> (i % NS)) & 1u, z)) {
+                const bool raise = logits(sb, (valid >> (i % NS)) & 1u, z);
+                keep_logits(w0 + (int64_t)i * RPS + r, z);
+                if (raise) {
                     grew = true;
                     break;
                 }
@@ -610,7 +640,7 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         }
         const int gl = (int)blockIdx.z * HG + g;       // head within the KV group
         if (sub == 0) {
-            if (nsplit == 1) {
+            if (!ACC && nsplit == 1) {
                 float *po = out + ((int64_t)b * Hq + gq0 + g) * D + cc;
                 const float inv = Lsum > 0.f ? 1.f / Lsum : 0.f;
                 if ((reinterpret_cast<uintptr_t>(po) & 15u) == 0) {
@@ -719,10 +749,12 @@ static int64_t plan_split_rows(int64_t wgs_per_split, int64_t max_rows, int page
     return ceil_div(rows, page_size) * page_size;
 }
 
+// acc: the weights of sg_decode_attn_acc, or NULL.
 template <typename T, int D, int G>
 static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, float scale_log2, const void *q,
                          const void *k_pool, const void *v_pool, int64_t pool_rows, const int32_t *page_table,
-                         const int32_t *n_rows, int page_size, int max_pages, float *out, float *ws, size_t ws_bytes) {
+                         const int32_t *n_rows, int page_size, int max_pages, float *out, float *ws, size_t ws_bytes,
+                         const Weights *acc) {
     constexpr int HG = G < DEC_MAX_HG ? G : DEC_MAX_HG;
     constexpr int NHG = G / HG;
     constexpr int WAVES = DecodeShape<T, D, HG>::WAVES;
@@ -740,9 +772,12 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
         set_error("%s: %lld splits of %lld rows are not supported", fn, (long long)nsplit, (long long)split_rows);
         return SG_EUNSUPPORTED;
     }
-    const size_t need = nsplit > 1 ? (size_t)units * nsplit * G * (D + 2) * sizeof(float) : 0;
+    const size_t zfloats = acc ? (size_t)units * G * z_stride_of(max_rows) : 0;
+    const size_t need = (acc || nsplit > 1 ? (size_t)units * nsplit * G * (D + 2) * sizeof(float) : 0) +
+                        zfloats * sizeof(float);
     if (need > ws_bytes || (need && !ws)) {
-        set_error("%s: the split states need %zu bytes of workspace, %zu given", fn, need, ws_bytes);
+        set_error("%s: the split states%s need %zu bytes of workspace, %zu given", fn,
+                  acc ? " and logits" : "", need, ws_bytes);
         return SG_EWORKSPACE;
     }
     // division by the page size as a multiply-shift, exact for dividends below
@@ -757,10 +792,24 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
     if (parts)
         grid = dim3((unsigned)(DEC_XCDS * DEC_ENGINES *
                                ceil_div(ceil_div(units, DEC_XCDS), DEC_ENGINES / DEC_PARTS)), 1, 1);
-    decode_kernel<T, D, HG><<<grid, 64 * WAVES, 0, s>>>(
-        Hq, Hkv, scale_log2, reinterpret_cast<const T *>(q), reinterpret_cast<const v4u *>(k_pool),
-        reinterpret_cast<const v4u *>(v_pool), pool_rows, page_table, n_rows, page_size, page_mul, page_shift,
-        max_pages, split_rows, out, ws, (int)units, parts ? DEC_PARTS : 0);
+    auto launch = [&](auto kernel, float *states, float *z, int64_t z_stride) {
+        kernel<<<grid, 64 * WAVES, 0, s>>>(
+            Hq, Hkv, scale_log2, reinterpret_cast<const T *>(q), reinterpret_cast<const v4u *>(k_pool),
+            reinterpret_cast<const v4u *>(v_pool), pool_rows, page_table, n_rows, page_size, page_mul, page_shift,
+            max_pages, split_rows, out, states, (int)units, parts ? DEC_PARTS : 0, z, z_stride);
+    };
+    if (acc) {
+        Weights w = *acc;
+        w.z = ws;
+        w.z_stride = z_stride_of(max_rows);
+        float *states = ws + zfloats;
+        launch(decode_kernel<T, D, HG, true>, states, w.z, w.z_stride);
+        const dim3 fgrid((unsigned)units, (unsigned)ceil_div(max_rows, FINISH_ROWS));
+        decode_finish_kernel<D><<<fgrid, FINISH_THREADS, 0, s>>>(Hq, Hkv, (int)nsplit, n_rows, max_rows, split_rows,
+                                                                 states, out, w);
+        return launch_status(fn);
+    }
+    launch(decode_kernel<T, D, HG, false>, ws, nullptr, 0);
     if (nsplit > 1)
         decode_merge_kernel<D, G><<<(unsigned)units, 256, 0, s>>>(Hq, Hkv, (int)nsplit, n_rows, max_rows, split_rows, ws,
                                                                   out);
@@ -770,13 +819,13 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
 template <typename T, int D>
 static int dispatch_g(const char *fn, int G, hipStream_t s, int B, int Hq, int Hkv, float sl2, const void *q, const void *kp,
                       const void *vp, int64_t pr, const int32_t *pt, const int32_t *nr, int ps, int mp, float *out,
-                      float *ws, size_t wsb) {
+                      float *ws, size_t wsb, const Weights *acc) {
     switch (G) {
-        case 1: return launch_decode<T, D, 1>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb);
-        case 2: return launch_decode<T, D, 2>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb);
-        case 4: return launch_decode<T, D, 4>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb);
-        case 8: return launch_decode<T, D, 8>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb);
-        case 16: return launch_decode<T, D, 16>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb);
+        case 1: return launch_decode<T, D, 1>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb, acc);
+        case 2: return launch_decode<T, D, 2>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb, acc);
+        case 4: return launch_decode<T, D, 4>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb, acc);
+        case 8: return launch_decode<T, D, 8>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb, acc);
+        case 16: return launch_decode<T, D, 16>(fn, s, B, Hq, Hkv, sl2, q, kp, vp, pr, pt, nr, ps, mp, out, ws, wsb, acc);
         default: set_error("%s: group size %d not supported (1, 2, 4, 8, 16)", fn, G); return SG_EUNSUPPORTED;
     }
 }
@@ -786,7 +835,7 @@ static int dispatch_g(const char *fn, int G, hipStream_t s, int B, int Hq, int H
 static int decode_attn_call(const char *fn, void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d, float scale,
                             const void *q, const void *k_pool, const void *v_pool, int64_t pool_rows,
                             const int32_t *page_table, const int32_t *n_rows, int page_size, int max_pages,
-                            float *out, void *ws, size_t ws_bytes) {
+                            float *out, void *ws, size_t ws_bytes, const Weights *acc = nullptr) {
     SG_REQUIRE(dt == SG_F32 || dt == SG_BF16, SG_EINVAL, "%s: unknown dtype %d", fn, (int)dt);
     SG_REQUIRE(B >= 0 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0, SG_EINVAL,
                "%s: need Hq %% Hkv == 0 (Hq=%d, Hkv=%d)", fn, Hq, Hkv);
@@ -805,11 +854,11 @@ static int decode_attn_call(const char *fn, void *stream, sg_dtype dt, int B, in
     hipStream_t s = as_stream(stream);
     float *w = reinterpret_cast<float *>(ws);
     if (dt == SG_F32) {
-        if (d == 64) return dispatch_g<float, 64>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes);
-        return dispatch_g<float, 128>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes);
+        if (d == 64) return dispatch_g<float, 64>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes, acc);
+        return dispatch_g<float, 128>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes, acc);
     }
-    if (d == 64) return dispatch_g<uint16_t, 64>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes);
-    return dispatch_g<uint16_t, 128>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes);
+    if (d == 64) return dispatch_g<uint16_t, 64>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes, acc);
+    return dispatch_g<uint16_t, 128>(fn, G, s, B, Hq, Hkv, sl2, q, k_pool, v_pool, pool_rows, page_table, n_rows, page_size, max_pages, out, w, ws_bytes, acc);
 }
 
 // Split states of sg_decode_attn_noalloc: a file-scope device array, one copy
@@ -877,4 +926,28 @@ extern "C" int sg_decode_attn_noalloc(void *stream, sg_dtype dt, int B, int Hq, 
     if (!ws) return SG_EHIP;
     return decode_attn_call("sg_decode_attn_noalloc", stream, dt, B, Hq, Hkv, d, scale, q, k_pool, v_pool, pool_rows,
                             page_table, n_rows, page_size, max_pages, out, ws, DEC_SCRATCH_BYTES);
+}
+
+extern "C" size_t sg_decode_attn_acc_workspace_size(int B, int Hq, int Hkv, int d, int max_pages, int page_size) {
+    if (B <= 0 || Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || d <= 0 || max_pages <= 0 || page_size <= 0) return 0;
+    const int64_t max_rows = (int64_t)max_pages * page_size;
+    return (size_t)B * Hq * ((size_t)max_splits(max_rows) * (size_t)(d + 2) + (size_t)z_stride_of(max_rows)) *
+           sizeof(float);
+}
+
+extern "C" int sg_decode_attn_acc(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d, float scale, const void *q,
+                                  const void *k_pool, const void *v_pool, int64_t pool_rows, const int32_t *page_table,
+                                  const int32_t *n_rows, int page_size, int max_pages, float *out,
+                                  const float *weight_in, float decay, float *weight_out, int64_t weight_stride,
+                                  void *ws, size_t ws_bytes) {
+    const char *fn = "sg_decode_attn_acc";
+    SG_REQUIRE(B == 0 || weight_out, SG_EINVAL, "%s: null weight_out", fn);
+    SG_REQUIRE(page_size >= 1 && max_pages >= 1 && weight_stride >= (int64_t)max_pages * page_size, SG_EINVAL,
+               "%s: weight rows of %lld floats hold no %d pages of %d rows", fn, (long long)weight_stride, max_pages,
+               page_size);
+    SG_REQUIRE(decay >= 0.f && decay <= 1.f, SG_EINVAL, "%s: decay must lie in [0, 1]", fn);
+    SG_REQUIRE(aligned16(ws), SG_EINVAL, "%s: the workspace must be 16-byte aligned", fn);
+    const Weights w{weight_in, weight_out, weight_stride, decay, nullptr, 0};
+    return decode_attn_call(fn, stream, dt, B, Hq, Hkv, d, scale, q, k_pool, v_pool, pool_rows, page_table, n_rows,
+                            page_size, max_pages, out, ws, ws_bytes, &w);
 }

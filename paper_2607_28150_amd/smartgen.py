@@ -17,7 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # SG_LIB_PATH points at another build of the same sources (the sanitizer run)
 LIB_PATH = os.environ.get("SG_LIB_PATH") or os.path.join(_HERE, "libsmartgen.so")
 
-SG_F32, SG_BF16 = 0, 1
+SG_F32, SG_BF16, SG_FP4 = 0, 1, 2
 SG_OK, SG_EINVAL, SG_EUNSUPPORTED, SG_EWORKSPACE, SG_EHIP, SG_EINTERNAL = 0, -1, -2, -3, -4, -5
 
 EXPORTS = [
@@ -33,6 +33,8 @@ EXPORTS = [
     "sg_fetch_keep", "sg_spec_quota", "sg_spec_push", "sg_spec_commit", "sg_score_count",
     "sg_decode_select_workspace_size", "sg_decode_select",
     "sg_score_topshare_workspace_size", "sg_score_topshare",
+    "sg_fetch_fp4", "sg_decode_attn_fp4_workspace_size", "sg_decode_attn_fp4",
+    "sg_decode_attn_acc_workspace_size", "sg_decode_attn_acc", "sg_evict_workspace_size", "sg_evict",
 ]
 
 
@@ -92,6 +94,22 @@ def load() -> ctypes.CDLL:
     lib.sg_spec_quota.restype = _l
     lib.sg_spec_push.argtypes = [_vp, _i, _i, _i, _i, _l, _l, _l, _i, _vp, _vp, _l, _vp, _vp, _l, _i, _vp, _vp, _vp]
     lib.sg_spec_commit.argtypes = [_vp, _i, _i, _l, _l, _l, _i, _i, _vp, _vp, _vp]
+    lib.sg_fetch_fp4.argtypes = [_vp, _i, _i, _i, _i, _vp, _l, _vp, _vp, _vp, _l, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp,
+                                 _vp, _vp, _l]
+    lib.sg_decode_attn_acc_workspace_size.argtypes = [_i] * 6
+    lib.sg_decode_attn_acc_workspace_size.restype = _sz
+    lib.sg_decode_attn_acc.argtypes = [_vp, _i, _i, _i, _i, _i, _f, _vp, _vp, _vp, _l, _vp, _vp, _i, _i, _vp, _vp, _f,
+                                       _vp, _l, _vp, _sz]
+    lib.sg_decode_attn_fp4_workspace_size.argtypes = [_i] * 7
+    lib.sg_decode_attn_fp4_workspace_size.restype = _sz
+    lib.sg_decode_attn_fp4.argtypes = [_vp, _i, _i, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _l, _vp, _vp, _i, _i, _vp, _vp,
+                                       _f, _vp, _l, _vp, _sz]
+    lib.sg_evict_workspace_size.argtypes = [_i] * 3
+    lib.sg_evict_workspace_size.restype = _sz
+    lib.sg_evict.argtypes = [_vp, _i, _i, _i, _vp, _vp, _vp, _l, _vp, _vp, _i, _i, _vp, _vp, _vp, _l, _i, _vp, _vp,
+                             _vp, _vp, _vp, _sz]
+    for f in ("sg_fetch_fp4", "sg_decode_attn_fp4", "sg_decode_attn_acc", "sg_evict"):
+        getattr(lib, f).restype = _i
     for f in ("sg_score", "sg_topk", "sg_pack", "sg_split", "sg_fetch", "sg_decode_attn", "sg_decode_attn_noalloc",
               "sg_block_importance",
               "sg_pack_blocks", "sg_fetch_keep", "sg_spec_push", "sg_spec_commit", "sg_score_count",
@@ -545,3 +563,164 @@ def sg_spec_commit(ids, L, Hkv, T, s0, N, M, mask, rem=None, stream=None):
     rc = load().sg_spec_commit(_stream(stream), int(L), int(Hkv), int(T), int(s0), int(N), int(M), ids.numel(),
                                _ptr(ids), _ptr(mask), _ptr(rem))
     _check("sg_spec_commit", rc)
+
+
+# ----------------------------------------------------------------------------- 4-bit rows
+
+def _here(*tensors):
+    """Device tensors of one call lie on the current device, where its kernels run."""
+    now = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+    for t in tensors:
+        _need(t is None or not t.is_cuda or t.device.index == now,
+              f"a tensor lies on {None if t is None else t.device}, the current device is {now}")
+
+
+def _row_code(k, v, s, d, what):
+    """Element type of K/V rows of d channels: uint8 codes with their scales, or f32 / bf16 without."""
+    _need(k.dtype == v.dtype, f"the K and V {what} differ in type")
+    if k.dtype != torch.uint8:
+        _need(s is None, f"{what}: scales go with uint8 codes only")
+        _need(v.numel() >= k.numel() // d * d, f"the V {what} is smaller than the K {what}")
+        return _dtype_code(k), k.numel() // d
+    rows = k.numel() // (d // 2)
+    _need(s is not None and s.dtype == torch.uint8, f"{what}: uint8 codes need uint8 scales [rows][2][d / 32]")
+    _need(v.numel() >= rows * (d // 2) and s.numel() >= rows * (d // 16),
+          f"the V codes or scales of the {what} are smaller than its K codes")
+    return SG_FP4, rows
+
+
+def _row_width(k):
+    return k.shape[-1] * (2 if k.dtype == torch.uint8 else 1)
+
+
+def _int32(t, n, what):
+    _need(t.dtype == torch.int32 and t.numel() >= n, f"{what} must be int32 with {n} entries")
+
+
+def sg_fetch_fp4(row_off, total, index, n_valid, src_row_base, k_src, v_src, page_table, page_size, dst_start,
+                 k_pool, v_pool, s_src=None, s_pool=None, stream=None):
+    """sg_fetch into or out of 4-bit rows: uint8 codes [..., d / 2] with scales
+    [..., 2, d / 32] on the source side (s_src), the pool's (s_pool) or both; the
+    other side float32 or bfloat16 rows of d."""
+    rows = row_off.numel() - 1
+    d = _row_width(k_src)
+    _need(_row_width(k_pool) == d, "source and pool rows differ in width")
+    src_dt, src_rows = _row_code(k_src, v_src, s_src, d, "source")
+    dst_dt, pool_rows = _row_code(k_pool, v_pool, s_pool, d, "pool")
+    max_pages = page_table.shape[-1]
+    _int32(row_off, 1, "row_off")
+    _int32(page_table, rows * max_pages, "page_table")
+    _int32(dst_start, rows, "dst_start")
+    _need(src_row_base.dtype == torch.int64 and src_row_base.numel() >= rows, "src_row_base must be int64 [rows]")
+    if n_valid is not None:
+        _int32(n_valid, rows, "n_valid")
+    if index is not None:
+        _int32(index, total, "index")
+    _here(row_off, index, n_valid, src_row_base, k_src, v_src, s_src, page_table, dst_start, k_pool, v_pool, s_pool)
+    rc = load().sg_fetch_fp4(_stream(stream), src_dt, dst_dt, d, rows, _ptr(row_off), int(total), _ptr(index),
+                             _ptr(n_valid), _ptr(src_row_base), src_rows, _ptr(k_src), _ptr(v_src), _ptr(s_src),
+                             _ptr(page_table), int(page_size), int(max_pages), _ptr(dst_start), _ptr(k_pool),
+                             _ptr(v_pool), _ptr(s_pool), pool_rows)
+    _check("sg_fetch_fp4", rc)
+
+
+# ----------------------------------------------------------------------------- accumulated weights and eviction
+
+def decode_acc_workspace_size(B, Hq, Hkv, d, max_pages, page_size) -> int:
+    return int(load().sg_decode_attn_acc_workspace_size(B, Hq, Hkv, d, max_pages, page_size))
+
+
+def decode_fp4_workspace_size(B, Hq, Hkv, d, max_pages, page_size, weights=False) -> int:
+    return int(load().sg_decode_attn_fp4_workspace_size(B, Hq, Hkv, d, max_pages, page_size, int(bool(weights))))
+
+
+def _decode_shape(q, page_table, n_rows, out, page_size, weight, weight_out):
+    B, Hq, d = q.shape
+    _need(page_table.dim() == 3 and page_table.shape[0] == B, "page_table must be [B][Hkv][max_pages]")
+    Hkv, max_pages = page_table.shape[1], page_table.shape[2]
+    _need(Hkv > 0 and Hq % Hkv == 0, "Hq must be a multiple of Hkv")
+    _int32(page_table, 0, "page_table")
+    _int32(n_rows, B * Hkv, "n_rows")
+    _need(out.dtype == torch.float32 and out.numel() >= B * Hq * d, "out must be float32 [B][Hq][d]")
+    stride = 0
+    if weight_out is not None:
+        stride = weight_out.shape[-1]
+        _need(stride >= max_pages * page_size, "weights must hold max_pages * page_size rows")
+    for w in (weight, weight_out):
+        _need(w is None or (w.dtype == torch.float32 and w.shape[-1] == stride and w.numel() >= B * Hkv * stride),
+              "weights must be float32 [B][Hkv][rows]")
+    return B, Hq, Hkv, d, max_pages, stride
+
+
+def sg_decode_attn_acc(q, k_pool, v_pool, page_table, n_rows, page_size, out, weight_out, ws, weight=None, decay=1.0,
+                       scale=None, stream=None):
+    """sg_decode_attn that also writes weight_out [B][Hkv][rows] = decay * weight +
+    the probability each row received, summed over its q heads (weight=None: zeros;
+    weight_out may be weight)."""
+    B, Hq, Hkv, d, max_pages, stride = _decode_shape(q, page_table, n_rows, out, page_size, weight, weight_out)
+    _need(k_pool.dtype == q.dtype and v_pool.dtype == q.dtype, "q and pools must share a dtype")
+    pool_rows = k_pool.numel() // d
+    _need(v_pool.numel() >= pool_rows * d, "v_pool smaller than k_pool")
+    _here(q, k_pool, v_pool, page_table, n_rows, out, weight, weight_out, ws)
+    rc = load().sg_decode_attn_acc(_stream(stream), _dtype_code(q), B, Hq, Hkv, d,
+                                   float(d ** -0.5 if scale is None else scale), _ptr(q), _ptr(k_pool), _ptr(v_pool),
+                                   pool_rows, _ptr(page_table), _ptr(n_rows), int(page_size), max_pages, _ptr(out),
+                                   _ptr(weight), float(decay), _ptr(weight_out), stride, _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size())
+    _check("sg_decode_attn_acc", rc)
+    return out
+
+
+def sg_decode_attn_fp4(q, k_pool, v_pool, s_pool, page_table, n_rows, page_size, out, ws=None, scale=None,
+                       weight=None, weight_out=None, decay=1.0, stream=None):
+    """out[B][Hq][d] (float32) = attention of q [B][Hq][d] (float32 or bfloat16) over
+    the paged set of 4-bit rows: codes [rows][d / 2], scales [rows][2][d / 32].  With
+    weight_out, the rows' weights as sg_decode_attn_acc."""
+    B, Hq, Hkv, d, max_pages, stride = _decode_shape(q, page_table, n_rows, out, page_size, weight, weight_out)
+    code, pool_rows = _row_code(k_pool, v_pool, s_pool, d, "pool")
+    _need(code == SG_FP4 and _row_width(k_pool) == d, "the pools must be uint8 codes [rows][d / 2]")
+    _here(q, k_pool, v_pool, s_pool, page_table, n_rows, out, weight, weight_out, ws)
+    rc = load().sg_decode_attn_fp4(_stream(stream), _dtype_code(q), B, Hq, Hkv, d,
+                                   float(d ** -0.5 if scale is None else scale), _ptr(q), _ptr(k_pool), _ptr(v_pool),
+                                   _ptr(s_pool), pool_rows, _ptr(page_table), _ptr(n_rows), int(page_size), max_pages,
+                                   _ptr(out), _ptr(weight), float(decay), _ptr(weight_out), stride, _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size())
+    _check("sg_decode_attn_fp4", rc)
+    return out
+
+
+def evict_workspace_size(units, max_pages, page_size) -> int:
+    return int(load().sg_evict_workspace_size(int(units), int(max_pages), int(page_size)))
+
+
+def sg_evict(k_pool, v_pool, page_table, n_rows, page_size, budget, weight, n_kept, weight_out, ws, pos=None,
+             pos_out=None, sinks=0, recent_from=None, s_pool=None, stream=None):
+    """Cuts every unit's paged set (page_table [..., max_pages], n_rows and budget one
+    entry per unit) to min(budget, n_rows) rows by weight [units][rows]; kept rows past
+    the new count move into the holes before it, with their weights and positions.
+    n_kept, weight_out and pos_out may be n_rows, weight and pos."""
+    max_pages = page_table.shape[-1]
+    units = page_table.numel() // max_pages
+    d = _row_width(k_pool)
+    dt, pool_rows = _row_code(k_pool, v_pool, s_pool, d, "pool")
+    stride = weight.shape[-1]
+    _int32(page_table, 0, "page_table")
+    for t, what in ((n_rows, "n_rows"), (budget, "budget"), (n_kept, "n_kept")):
+        _int32(t, units, what)
+    if recent_from is not None:
+        _int32(recent_from, units, "recent_from")
+    _need(stride >= max_pages * page_size, "weights must hold max_pages * page_size rows")
+    for w in (weight, weight_out):
+        _need(w.dtype == torch.float32 and w.shape[-1] == stride and w.numel() >= units * stride,
+              "weight and weight_out must be float32 [units][rows]")
+    _need((pos is None) == (pos_out is None), "pos and pos_out go together")
+    for p in (pos, pos_out):
+        _need(p is None or (p.dtype == torch.int32 and p.shape[-1] == stride and p.numel() >= units * stride),
+              "pos and pos_out must be int32 like weight")
+    _here(k_pool, v_pool, s_pool, page_table, n_rows, budget, weight, pos, recent_from, n_kept, weight_out, pos_out, ws)
+    rc = load().sg_evict(_stream(stream), dt, units, d, _ptr(k_pool), _ptr(v_pool), _ptr(s_pool), pool_rows,
+                         _ptr(page_table), _ptr(n_rows), int(page_size), max_pages, _ptr(budget), _ptr(weight),
+                         _ptr(pos), stride, int(sinks), _ptr(recent_from), _ptr(n_kept), _ptr(weight_out),
+                         _ptr(pos_out), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    _check("sg_evict", rc)
+    return n_kept
