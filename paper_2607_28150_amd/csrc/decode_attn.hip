@@ -806,7 +806,7 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
         launch(decode_kernel<T, D, HG, true>, states, w.z, w.z_stride);
         const dim3 fgrid((unsigned)units, (unsigned)ceil_div(max_rows, FINISH_ROWS));
         decode_finish_kernel<D><<<fgrid, FINISH_THREADS, 0, s>>>(Hq, Hkv, (int)nsplit, n_rows, max_rows, split_rows,
-                                                                 states, out, w);
+                                                                 nullptr, states, out, w);
         return launch_status(fn);
     }
     launch(decode_kernel<T, D, HG, false>, ws, nullptr, 0);

@@ -31,8 +31,9 @@ struct Weights {
     int64_t z_stride;
 };
 
-// Floats of a head's logits of a unit in the workspace.
-inline int64_t z_stride_of(int64_t max_rows) { return ceil_div(max_rows, 4) * 4; }
+// Floats of a head's logits of a unit in the workspace (whole tiles of 32, so
+// that a tile is stored without a look at its rows).
+inline int64_t z_stride_of(int64_t max_rows) { return ceil_div(max_rows, 32) * 32; }
 
 // Splits of a unit of n rows that wrote a state (split_rows == 0: equal parts).
 __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_rows) {
@@ -40,18 +41,27 @@ __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_
 }
 
 // Grid: x = unit, y = chunk of FINISH_ROWS rows (chunk 0 also writes the
-// unit's outputs).
+// unit's outputs).  States of a unit: nsplit places, of which the used ones come
+// first; or, with `spans`, places unit + spans[unit].x .. unit + spans[unit].y,
+// where a unit with one state and no weights has its output already.
 template <int D>
 static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
     int Hq, int Hkv, int nsplit, const int32_t *__restrict__ n_rows, int64_t max_rows, int64_t split_rows,
-    const float *__restrict__ states, float *__restrict__ out, Weights w) {
+    const int2 *__restrict__ spans, const float *__restrict__ states, float *__restrict__ out, Weights w) {
     __shared__ float M[FINISH_MAX_G], inv[FINISH_MAX_G];
     const int G = Hq / Hkv;
     const int64_t unit = blockIdx.x;
     const int64_t n = max<int64_t>(0, min<int64_t>(n_rows[unit], max_rows));
     if (blockIdx.y > 0 && (int64_t)blockIdx.y * FINISH_ROWS >= n) return;      // uniform
-    const int used = used_splits(n, nsplit, split_rows);
-    const float *st = states + unit * nsplit * G * (int64_t)(D + 2);
+    int used = used_splits(n, nsplit, split_rows);
+    int64_t first = unit * nsplit;
+    if (spans && n > 0) {
+        const int2 sp = spans[unit];
+        if (sp.x == sp.y && !w.out) return;      // uniform
+        used = sp.y - sp.x + 1;
+        first = unit + sp.x;
+    }
+    const float *st = states + first * G * (int64_t)(D + 2);
     const int lane = threadIdx.x % 64;
     for (int g = threadIdx.x / 64; g < G; g += FINISH_THREADS / 64) {
         float m = -INFINITY, l = 0.f;

@@ -100,7 +100,7 @@ def test_decode_fp4_rejections(lib):
     assert call(pages=1024, ws=None, wsb=0) == sg.SG_EWORKSPACE
     assert call(B=0) == sg.SG_OK
     assert sg.decode_fp4_workspace_size(1, 32, 8, 128, 1, 16) == 0          # one split, no weights
-    assert sg.decode_fp4_workspace_size(1, 32, 8, 128, 1, 16, weights=True) == 32 * (130 + 16) * 4
+    assert sg.decode_fp4_workspace_size(1, 32, 8, 128, 1, 16, weights=True) == 32 * (130 + 32) * 4
     assert sg.decode_fp4_workspace_size(0, 32, 8, 128, 1, 16, weights=True) == 0
 
 
@@ -118,7 +118,7 @@ def test_decode_acc_rejections(lib):
     assert call(wsb=64) == sg.SG_EWORKSPACE
     assert call(ws=ctypes.c_void_p(8)) == sg.SG_EINVAL
     assert call(pages=0) == sg.SG_EINVAL
-    assert sg.decode_acc_workspace_size(1, 32, 8, 128, 1, 16) == 32 * (130 + 16) * 4
+    assert sg.decode_acc_workspace_size(1, 32, 8, 128, 1, 16) == 32 * (130 + 32) * 4
 
 
 def test_evict_rejections(lib):
