@@ -1,22 +1,25 @@
 // sg_decode_attn_fp4: GQA decode attention over a paged set of 4-bit rows
 // (fp4.h), with or without the weights the rows receive (decode_weights.h).
 //
-// Work.  Every (sequence, KV head) unit is cut into tiles of 32 rows.  Where the
-// units are few enough for their lengths to leave the chip uneven, the tiles of
-// all units stand in one line and D4_WGS workgroups (two per CU, all resident)
-// take equal shares of it: a share covers the end of one unit, whole units, the
-// start of another, and leaves a state per unit it touches; a second launch
-// joins the states.  With more units a workgroup takes a whole one.  A
-// workgroup's four wavefronts take its tiles in turn and serve all G <= 16
-// query heads of the unit.
+// Work.  Every (sequence, KV head) unit is cut into tiles of 32 rows, and the
+// tiles of all units stand in one line, of which up to D4_SHARES wavefronts
+// (eight per CU, all resident) take equal shares: the end of one unit, whole
+// units, the start of another.  A wavefront serves all G <= 16 query heads of a
+// unit and leaves a state for every unit it touches; a second launch joins
+// them.  Wavefronts are workgroups of their own: nothing waits for another, and
+// the loads run on across the units of a share.  (Workgroups of four wavefronts
+// that shared a unit's rows and met at its end: 64 requests 66 us, 16 long
+// prompts 82.)  More units than one lookup covers: a wavefront takes a whole one.
 //
-// Memory.  A wavefront streams its tiles through a private LDS ring with direct
-// global->LDS loads, NS - 1 tiles ahead of its arithmetic: codes of 16 K and 16
-// V rows per instruction (d = 128), the tile's scales in one more.  A lane may
-// fetch any row into its place of the ring, so the places are chosen for the
-// reads: K's 16-byte pieces rotated against the bank conflicts of whole rows,
-// V's rows in the order 0, 4, 8, 12, 1, ... in which four quarters of a
-// wavefront read them.
+// Memory.  A wavefront streams its tiles through an LDS ring with direct
+// global->LDS loads, NS - 1 tiles ahead of its arithmetic, the tiles' page
+// entries another NS - 1 tiles ahead of those: codes of 16 K and 16 V rows per
+// instruction (d = 128), the tile's scales in one more.  Every step issues the
+// same loads, so one constant counter wait covers a tile's rows and the page
+// entries that are due with it.  A lane may fetch any row into its place of
+// the ring, so the places are chosen for the reads: K's 16-byte pieces rotated
+// against the bank conflicts of whole rows, V's rows in the order 0, 4, 8, 12,
+// 1, ... in which four quarters of a wavefront read them.
 //
 // Arithmetic.  Matrix instructions (16 x 16 x 32, bf16 in, fp32 out):
 //   logits : A = 16 K rows x 32 channels, B = the same channels of 16 heads.
@@ -42,15 +45,14 @@ namespace sg {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));     // outputs may start at any float
 
-constexpr int D4_WAVES = 4;
-constexpr int D4_THREADS = 64 * D4_WAVES;
-constexpr int D4_TILE = 32;                  // rows per wavefront and step
-constexpr int D4_NS = 4;                     // ring slots per wavefront
-constexpr int D4_PT_CAP = 2048;              // page entries staged in LDS at a time
+constexpr int D4_TILE = 32;                  // rows per step
+constexpr int D4_NS = 4;                     // ring slots
 constexpr float D4_LAZY = 16.f;              // log2 headroom before the reference max is raised
-constexpr int D4_WGS = 512;                  // workgroups that share the tiles of all units
-constexpr int D4_SHARED_UNITS = 8 * D4_THREADS;      // most units shared that way
+constexpr int D4_SHARES = 2048;              // wavefronts that share the tiles of all units
+constexpr int D4_MIN_SHARE = 2;              // tiles of a share at least
+constexpr int D4_SHARED_UNITS = 64 * 64;     // most units shared that way
 
 // One ring slot: a tile's K codes, V codes and scales.
 template <int D>
@@ -58,7 +60,7 @@ struct Tile4 {
     static constexpr int CODES = D4_TILE * D / 2;
     static constexpr int SB = 2 * D / FP4_BLOCK;     // scale bytes per row: K's, then V's
     static constexpr int SLOT = 2 * CODES + 256;
-    static constexpr int LOADS = 2 * CODES / 1024 + 1;
+    static constexpr int LOADS = 2 * CODES / 1024 + 2;     // of a step, page entries included
 };
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const v4u &w) {
@@ -80,6 +82,9 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { retu
 
 // Direct global->LDS load of 4 bytes per lane: lane i's land at LDS offset
 // lds + 4 i (see dma16 in sg_internal.h).
+__device__ __forceinline__ void dma4(const void *src, unsigned lds) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(lds) : "memory");
+}
 __device__ __forceinline__ void dma4_nt(const void *src, unsigned lds) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off nt" ::"v"(src), "{m0}"(lds) : "memory");
 }
@@ -95,96 +100,153 @@ struct Decode4Args {
     uint32_t page_mul;
     int page_shift;
     float *out, *states;
-    int2 *spans;           // per unit: first and last workgroup that left a state (shared tiles)
+    int2 *spans;           // per unit: first and last wavefront that left a state (shared tiles)
     float *z;              // logits [units][G][z_stride], or unused
     int64_t z_stride;
 };
 
+// A place in a share: tile `tile` of unit `unit` (n rows); `left` tiles of the
+// share from here on.
+struct Cursor4 {
+    int unit, tile, n, left;
+};
+
 // T: type of the queries; KEEP: the logits are kept for the weights and every
-// unit leaves a state; SHARED: workgroups share the tiles of all units.
+// unit leaves a state; SHARED: wavefronts share the tiles of all units.
 template <typename T, int D, bool KEEP, bool SHARED>
-__global__ __launch_bounds__(D4_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void decode4_kernel(Decode4Args a) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void decode4_kernel(Decode4Args a) {
     using L = Tile4<D>;
     constexpr int STEPS = D / 32;            // K products per 16 rows: 8 channels of every lane each
     constexpr int NC = D / 16;               // V channels per lane, and products per 32 rows
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     constexpr int NS = D4_NS, SB = L::SB;
-    static_assert((NS - 1) * L::LOADS <= 63, "loads in flight per wavefront");
-    static_assert(NS * L::SLOT >= 16 * D * 4, "a wavefront's state fits its ring");
-    __shared__ __attribute__((aligned(16))) char ring[D4_WAVES * NS * L::SLOT];
-    __shared__ int32_t pte[D4_PT_CAP];
-    __shared__ float m_s[D4_WAVES][16], l_s[D4_WAVES][16];
+    static_assert((NS - 1) * L::LOADS <= 63, "loads in flight");
+    __shared__ __attribute__((aligned(16))) char ring[NS * L::SLOT];
+    __shared__ int32_t entries[NS][64];      // page entries of a tile's rows (each twice)
 
-    const int tid = threadIdx.x, lane = tid % 64, n16 = lane % 16, kg = lane / 16;
-    const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int lane = threadIdx.x, n16 = lane % 16, kg = lane / 16;
     const int Hq = a.Hq, Hkv = a.Hkv, G = Hq / Hkv, page_size = a.page_size;
     const int64_t max_rows = (int64_t)a.max_pages * page_size;
-    auto rows_of = [&](int64_t u) { return (int)max<int64_t>(0, min<int64_t>((int64_t)a.n_rows[u], max_rows)); };
-
-    // the first unit and tile, and the number of tiles of this workgroup
-    int64_t unit = blockIdx.x, left = 1;
-    int tile = 0;
-    if constexpr (SHARED) {
-        __shared__ int64_t wsum[D4_WAVES];
-        __shared__ int first_unit, first_tile;
-        // thread t holds units [t * per, (t + 1) * per)
-        const int per = (int)ceil_div(a.units, D4_THREADS);       // at most 8
-        int count[8];
-        int64_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int u = tid * per + i;
-            count[i] = i < per && u < a.units ? (rows_of(u) + D4_TILE - 1) / D4_TILE : 0;
-            mine += count[i];
-        }
-        int64_t scan = mine;
+    auto rows_of = [&](int u) { return (int)max<int64_t>(0, min<int64_t>((int64_t)a.n_rows[u], max_rows)); };
+    auto tiles_of = [](int n) { return (n + D4_TILE - 1) / D4_TILE; };
+    auto scan64 = [&](int64_t x) {
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int64_t x = __shfl_up(scan, o, 64);
-            scan += lane >= o ? x : 0;
+            const int64_t y = __shfl_up(x, o, 64);
+            x += lane >= o ? y : 0;
         }
-        if (lane == 63) wsum[wave] = scan;
-        __syncthreads();
-        int64_t total = 0, before = scan - mine;
+        return x;
+    };
+
+    Cursor4 cur{(int)blockIdx.x, 0, 0, 0};
+    int near = 0, n_near = 0;                // lane i: rows of unit near + i
+    if constexpr (SHARED) {
+        // The tile this share starts with: lane t sums the tiles of units
+        // [t * per, (t + 1) * per); the lane whose range holds it, then the unit.
+        const int per = (a.units + 63) / 64;         // at most 64
+        int64_t mine = 0;
+        for (int i0 = 0; i0 < per; i0 += 8) {
+            int c[8];
 #pragma unroll
-        for (int w = 0; w < D4_WAVES; ++w) {
-            before += w < wave ? wsum[w] : 0;
-            total += wsum[w];
-        }
-        // a tile at least for every wavefront (and never a share without a tile:
-        // a unit's states lie side by side)
-        const int64_t shares = max<int64_t>(1, min<int64_t>(gridDim.x, total / D4_WAVES));
-        const int64_t p0 = total * blockIdx.x / shares, p1 = total * (blockIdx.x + 1) / shares;
-        if (blockIdx.x >= shares || total == 0) return;      // uniform
-        left = p1 - p0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (p0 >= before && p0 < before + count[i]) {
-                first_unit = tid * per + i;
-                first_tile = (int)(p0 - before);
+            for (int i = 0; i < 8; ++i) {
+                const int u = lane * per + i0 + i;
+                c[i] = a.n_rows[min(u, a.units - 1)];
             }
-            before += count[i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int u = lane * per + i0 + i;
+                const int n = (int)max<int64_t>(0, min<int64_t>(c[i], max_rows));
+                mine += i0 + i < per && u < a.units ? tiles_of(n) : 0;
+            }
         }
-        __syncthreads();
-        unit = __builtin_amdgcn_readfirstlane(first_unit);
-        tile = __builtin_amdgcn_readfirstlane(first_tile);
+        const int64_t upto = scan64(mine);
+        const int64_t total = __shfl(upto, 63, 64);
+        // (never a share without a tile: a unit's states lie side by side)
+        const int64_t shares = max<int64_t>(1, min<int64_t>(gridDim.x, total / D4_MIN_SHARE));
+        if (blockIdx.x >= shares || total == 0) return;
+        const int64_t p0 = total * blockIdx.x / shares, p1 = total * (blockIdx.x + 1) / shares;
+        const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < upto)) - 1);
+        const int64_t before = __shfl(upto - mine, at, 64);
+        near = at * per;
+        n_near = near + lane < a.units ? rows_of(near + lane) : 0;
+        const int t = lane < per ? tiles_of(n_near) : 0;
+        const int64_t end = before + scan64(t);
+        const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < end)) - 1);
+        cur.unit = near + i;
+        cur.n = __builtin_amdgcn_readlane(n_near, i);
+        cur.tile = __builtin_amdgcn_readfirstlane((int)(p0 - __shfl(end - t, i, 64)));
+        cur.left = __builtin_amdgcn_readfirstlane((int)(p1 - p0));
+    } else {
+        cur.n = rows_of(cur.unit);
+        cur.left = tiles_of(cur.n);
     }
+    auto advance = [&](Cursor4 &c) {
+        if (--c.left <= 0) return;           // past the share it stays where it is
+        if (++c.tile * D4_TILE < c.n) return;
+        c.tile = 0;
+        do {
+            ++c.unit;                        // tiles are left, so units with rows are
+            c.n = c.unit - near < 64 ? __builtin_amdgcn_readlane(n_near, c.unit - near) : rows_of(c.unit);
+        } while (c.n == 0);
+    };
 
-    char *myring = ring + wave * (NS * L::SLOT);
-    for (; left > 0; ++unit, tile = 0) {
-        const int n = rows_of(unit), tiles = (n + D4_TILE - 1) / D4_TILE;
-        int tend = tiles;
-        if constexpr (SHARED) {
-            if (tiles == 0) continue;        // uniform
-            tend = (int)min<int64_t>(tiles, tile + left);
-            left -= tend - tile;
+    // Row of a tile that a lane stands for, its page and its place there
+    auto locate = [&](const Cursor4 &c, int &lr, uint32_t &page, int &off) {
+        lr = c.tile * D4_TILE + lane % 32;
+        const uint32_t in = (uint32_t)min(lr, c.n - 1);
+        page = (uint32_t)(((uint64_t)in * a.page_mul) >> a.page_shift);
+        off = (int)(in - page * (uint32_t)page_size);
+    };
+    auto issue_entries = [&](const Cursor4 &c, int slot) {
+        int lr, off;
+        uint32_t page;
+        locate(c, lr, page, off);
+        dma4(a.page_table + (int64_t)c.unit * a.max_pages + page, lds_addr(&entries[slot][0]));
+    };
+    // Loads of a tile's rows into a ring slot.  Lane i stands for row i % 32: its
+    // pool row goes round by lane permutes.  A row that is left out (past the
+    // unit's rows or the share, or outside the pool) reads pool row 0, its bit in
+    // `valid` is clear.
+    unsigned valid = 0u;
+    auto issue_rows = [&](const Cursor4 &c, int slot) {
+        int lr, off;
+        uint32_t page;
+        locate(c, lr, page, off);
+        const int64_t x = (int64_t)entries[slot][lane] + off;
+        const bool ok = c.left > 0 && lr < c.n && x >= 0 && x < a.pool_rows;
+        const int row = ok ? (int)x : 0;
+        valid = (valid & ~(1u << slot)) | ((ok ? 1u : 0u) << slot);
+        const unsigned base = lds_addr(ring + slot * L::SLOT);
+        if constexpr (D == 128) {
+            const int m4 = lane / 4, piece = lane % 4;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t kr = __shfl(row, 16 * u + m4, 64);
+                dma16_nt(a.k_pool + kr * 64 + (piece ^ (m4 / 4)) * 16, base + u * 1024);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t vr = __shfl(row, 16 * u + (m4 % 4) * 4 + m4 / 4, 64);
+                dma16_nt(a.v_pool + vr * 64 + piece * 16, base + L::CODES + u * 1024);
+            }
+            const int64_t sr = __shfl(row, lane / 2, 64);
+            dma4_nt(a.s_pool + sr * 8 + (lane % 2) * 4, base + 2 * L::CODES);
         } else {
-            left = 0;
+            const int p = lane / 2, piece = lane % 2;
+            const int64_t kr = __shfl(row, p, 64);
+            dma16_nt(a.k_pool + kr * 32 + piece * 16, base);
+            const int64_t vr = __shfl(row, (p / 16) * 16 + (p % 4) * 4 + (p % 16) / 4, 64);
+            dma16_nt(a.v_pool + vr * 32 + piece * 16, base + L::CODES);
+            dma4_nt(a.s_pool + (int64_t)row * 4, base + 2 * L::CODES);     // lanes 32 .. 63: the same again
         }
-        const int b = (int)(unit / Hkv), h = (int)(unit % Hkv);
+    };
 
-        // the queries: head n16, channels of quarter kg, 8 per product
-        bf16x8 qf[PARTS][STEPS];
+    bf16x8 qf[PARTS][STEPS];                 // head n16, channels of quarter kg, 8 per product
+    float m, l;                              // of head n16 (l: this lane's rows)
+    f32x4 o[NC];                             // o[j][i]: head 4 kg + i, channel NC n16 + j
+    int begun = cur.tile;                    // first tile taken of the current unit
+    auto begin_unit = [&](int unit) {
+        const int b = unit / Hkv, h = unit % Hkv;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             const T *qp = reinterpret_cast<const T *>(a.q) +
@@ -193,263 +255,224 @@ __global__ __launch_bounds__(D4_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             if constexpr (PARTS == 1) {
                 w[0] = *reinterpret_cast<const v4u *>(qp);
             } else {
+                const v4u x = *reinterpret_cast<const v4u *>(qp), y = *reinterpret_cast<const v4u *>(qp + 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t x[3], y[3];
-                    split3(qp[2 * i], x);
-                    split3(qp[2 * i + 1], y);
+                    uint32_t c[3], e[3];
+                    split3(__uint_as_float(i < 2 ? x[2 * i] : y[2 * i - 4]), c);
+                    split3(__uint_as_float(i < 2 ? x[2 * i + 1] : y[2 * i - 3]), e);
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) w[p][i] = high_halves(x[p], y[p]);
+                    for (int p = 0; p < 3; ++p) w[p][i] = high_halves(c[p], e[p]);
                 }
             }
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) qf[p][s] = as_bf16x8(n16 < G ? w[p] : v4u{0u, 0u, 0u, 0u});
         }
-        // waited for here: the compiler does not see the ring's loads and would
-        // drain them at the first use
+        // waited for here, once per unit: the compiler does not see the ring's
+        // loads and would otherwise drain them at every step
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) asm volatile("" ::"v"(qf[p][s]));
-
-        float m = -INFINITY, l = 0.f;        // of head n16 (l: this lane's rows)
-        f32x4 o[NC];                         // o[j][i]: head 4 kg + i, channel NC n16 + j
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        // As many tiles at a time as the staged page entries reach (all of them
-        // but for tiny pages), none of an empty pool.
-        const int reach = (int)min<int64_t>(1 << 26, (int64_t)(D4_PT_CAP - 2) * page_size / D4_TILE);
-        for (int c0 = tile; c0 < tend && a.pool_rows > 0; c0 += reach) {
-            const int c1 = min(tend, c0 + reach);
-            const int pg0 = c0 * D4_TILE / page_size;
-            const int npg = (min(n, c1 * D4_TILE) - 1) / page_size - pg0 + 1;
-            if (c0 > tile) __syncthreads();  // the entries before are no longer needed
-            for (int i = tid; i < npg; i += D4_THREADS) pte[i] = a.page_table[unit * a.max_pages + pg0 + i];
-            __syncthreads();
-
-            // Loads of tile t into a ring slot.  Lane i stands for row i % 32: its
-            // pool row goes round by lane permutes.  A row that is left out (past
-            // the unit's rows, or outside the pool) reads pool row 0, its bit in
-            // `valid` is clear.
-            unsigned valid = 0u;
-            auto issue = [&](int t, int slot) {
-                const int lr = t * D4_TILE + lane % 32;
-                const bool in = t < c1 && lr < n;
-                const uint32_t rel = in ? (uint32_t)(lr - pg0 * page_size) : 0u;
-                const uint32_t pi = (uint32_t)(((uint64_t)rel * a.page_mul) >> a.page_shift);
-                const int64_t x = (int64_t)pte[pi] + (int)(rel - pi * (uint32_t)page_size);
-                const bool ok = in && x >= 0 && x < a.pool_rows;
-                const int row = ok ? (int)x : 0;
-                valid = (valid & ~(1u << slot)) | ((ok ? 1u : 0u) << slot);
-                const unsigned base = lds_addr(myring + slot * L::SLOT);
-                if constexpr (D == 128) {
-                    const int m4 = lane / 4, piece = lane % 4;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int64_t kr = __shfl(row, 16 * u + m4, 64);
-                        dma16_nt(a.k_pool + kr * 64 + (piece ^ (m4 / 4)) * 16, base + u * 1024);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int64_t vr = __shfl(row, 16 * u + (m4 % 4) * 4 + m4 / 4, 64);
-                        dma16_nt(a.v_pool + vr * 64 + piece * 16, base + L::CODES + u * 1024);
-                    }
-                    const int64_t sr = __shfl(row, lane / 2, 64);
-                    dma4_nt(a.s_pool + sr * 8 + (lane % 2) * 4, base + 2 * L::CODES);
-                } else {
-                    const int p = lane / 2, piece = lane % 2;
-                    const int64_t kr = __shfl(row, p, 64);
-                    dma16_nt(a.k_pool + kr * 32 + piece * 16, base);
-                    const int64_t vr = __shfl(row, (p / 16) * 16 + (p % 4) * 4 + (p % 16) / 4, 64);
-                    dma16_nt(a.v_pool + vr * 32 + piece * 16, base + L::CODES);
-                    dma4_nt(a.s_pool + (int64_t)row * 4, base + 2 * L::CODES);     // lanes 32 .. 63: the same again
-                }
-            };
-            const int t0 = c0 + wave, steps = t0 < c1 ? (c1 - t0 + D4_WAVES - 1) / D4_WAVES : 0;
-            if (steps > 0) {
-#pragma unroll
-                for (int s = 0; s < NS - 1; ++s) issue(t0 + s * D4_WAVES, s);
-            }
-            for (int st = 0; st < steps; ++st) {
-                const int t = t0 + st * D4_WAVES, slot = st % NS;
-                issue(t + (NS - 1) * D4_WAVES, (st + NS - 1) % NS);
-                // the logits' stores count too: with them this waits for more than it needs
-                wait_vmem<(NS - 1) * L::LOADS>();
-                const char *sb = myring + slot * L::SLOT;
-                const uint8_t *sc = reinterpret_cast<const uint8_t *>(sb + 2 * L::CODES);
-                const uint32_t live = (uint32_t)__ballot((valid >> slot) & 1u);      // bit i: row i of the tile counts
-                // logits: lane (n16, kg) of half u gets rows 16 u + 4 kg + i of head n16
-                float z[8];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int row = 16 * u + n16;
-                    uint32_t kw[STEPS];
-                    uint32_t byte;
-                    if constexpr (D == 128) {
-                        const v4u x = *reinterpret_cast<const v4u *>(sb + row * 64 + ((kg ^ (n16 / 4)) * 16));
-#pragma unroll
-                        for (int s = 0; s < STEPS; ++s) kw[s] = x[s];
-                        byte = sc[row * SB + kg];
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(sb + row * 32 + kg * 8);
-                        kw[0] = x.x;
-                        kw[1] = x.y;
-                        byte = sc[row * SB + kg / 2];
-                    }
-                    const float ks = fp4_scale(byte);
-                    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) {
-                        const bf16x8 kf = as_bf16x8(v4u{fp4_bf16_pair<0>(kw[s], ks), fp4_bf16_pair<1>(kw[s], ks),
-                                                        fp4_bf16_pair<2>(kw[s], ks), fp4_bf16_pair<3>(kw[s], ks)});
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p)
-                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][s], acc, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i] * a.scale_log2;
-                }
-                if (live != 0xffffffffu) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        z[i] = (live >> (16 * (i / 4) + 4 * kg + i % 4)) & 1u ? z[i] : -INFINITY;
-                }
-                if constexpr (KEEP) {
-                    if (n16 < G) {
-                        float *zp = a.z + (unit * G + n16) * a.z_stride + (int64_t)t * D4_TILE + 4 * kg;
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-                            *reinterpret_cast<float4 *>(zp + 16 * u) =
-                                make_float4(z[4 * u], z[4 * u + 1], z[4 * u + 2], z[4 * u + 3]);
-                    }
-                }
-                float top = z[0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
-                if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
-                    top = fmaxf(top, __shfl_xor(top, 16, 64));
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const float mn = fmaxf(m, top);
-                    const float f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                    l *= f;
-                    m = mn;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float fi = __shfl(f, 4 * kg + i, 64);
-#pragma unroll
-                        for (int j = 0; j < NC; ++j) o[j][i] *= fi;
-                    }
-                }
-                const float ref = m == -INFINITY ? 0.f : m;
-                uint32_t pw[3][8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(z[i] - ref);
-                    l += p;
-                    uint32_t x[3];
-                    split3(p, x);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) pw[k][i] = x[k];
-                }
-                bf16x8 pf[3];
-#pragma unroll
-                for (int k = 0; k < 3; ++k)
-                    pf[k] = as_bf16x8(v4u{high_halves(pw[k][0], pw[k][1]), high_halves(pw[k][2], pw[k][3]),
-                                          high_halves(pw[k][4], pw[k][5]), high_halves(pw[k][6], pw[k][7])});
-                // values: 8 rows x NC channels per lane, as bf16 pairs of channels, then of rows
-                uint32_t vb[8][NC / 2];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int place = 16 * (i / 4) + 4 * (i % 4) + kg, row = 16 * (i / 4) + 4 * kg + i % 4;
-                    const char *vp = sb + L::CODES + place * (D / 2);
-                    uint32_t byte = sc[row * SB + SB / 2 + n16 * NC / FP4_BLOCK];
-                    // a row that is left out stands on pool row 0: its zero
-                    // probability must not meet a NaN
-                    if (live != 0xffffffffu) byte = (live >> row) & 1u ? byte : 0u;
-                    const float vs = fp4_scale(byte);
-                    uint32_t w;
-                    if constexpr (NC == 8) w = *reinterpret_cast<const uint32_t *>(vp + n16 * 4);
-                    else w = *reinterpret_cast<const uint16_t *>(vp + n16 * 2);
-                    vb[i][0] = fp4_bf16_pair<0>(w, vs);
-                    vb[i][1] = fp4_bf16_pair<1>(w, vs);
-                    if constexpr (NC == 8) {
-                        vb[i][2] = fp4_bf16_pair<2>(w, vs);
-                        vb[i][3] = fp4_bf16_pair<3>(w, vs);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < NC; ++j) {
-                    v4u w;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = __builtin_amdgcn_perm(vb[2 * i + 1][j / 2], vb[2 * i][j / 2],
-                                                     j % 2 == 0 ? 0x05040100u : 0x07060302u);
-                    const bf16x8 vf = as_bf16x8(w);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[k], vf, o[j], 0, 0, 0);
-                }
-            }
-            wait_vmem<0>();                  // the ring is reused
-        }
+    };
+    // The unit's state, or its outputs where this share held all of it.
+    auto end_unit = [&](int unit, bool last) {
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
-        if (kg == 0) {
-            m_s[wave][n16] = m;
-            l_s[wave][n16] = l;
+        const bool whole = !KEEP && begun == 0 && last;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t slot = SHARED ? (int64_t)unit + blockIdx.x : unit;   // both only go up: their sum numbers the states
+        float *st = a.states + slot * G * (D + 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int g = 4 * kg + i;
+            const float f = __shfl(inv, g, 64);
+            if (g >= G) continue;
+            float *p = whole ? a.out + ((int64_t)unit * G + g) * D + NC * n16 : st + g * (D + 2) + 2 + NC * n16;
+#pragma unroll
+            for (int j = 0; j < NC; j += 2)
+                *reinterpret_cast<f32x2u *>(p + j) = whole ? f32x2u{o[j][i] * f, o[j + 1][i] * f}
+                                                           : f32x2u{o[j][i], o[j + 1][i]};
         }
-        float *o_s = reinterpret_cast<float *>(myring);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < NC; ++j) o_s[(4 * kg + i) * D + NC * n16 + j] = o[j][i];
-        __syncthreads();
-        const bool whole = !KEEP && tile == 0 && tend == tiles;
-        for (int it = tid; it < G * D; it += D4_THREADS) {
-            const int g = it / D, c = it % D;
-            float M = -INFINITY, Ls = 0.f, O = 0.f;
-#pragma unroll
-            for (int w = 0; w < D4_WAVES; ++w) M = fmaxf(M, m_s[w][g]);
-#pragma unroll
-            for (int w = 0; w < D4_WAVES; ++w) {
-                const float f = m_s[w][g] == M ? 1.f : __builtin_amdgcn_exp2f(m_s[w][g] - M);
-                Ls += f * l_s[w][g];
-                O += f * reinterpret_cast<const float *>(ring + w * (NS * L::SLOT))[it];
-            }
-            if (whole) {
-                a.out[((int64_t)b * Hq + (int64_t)h * G + g) * D + c] = O * (Ls == 0.f ? 0.f : 1.f / Ls);
-            } else {
-                // shared tiles: a state per workgroup and unit it touches; both
-                // only go up, so their sum numbers the states
-                const int64_t slot = SHARED ? unit + blockIdx.x : unit;
-                float *p = a.states + (slot * G + g) * (int64_t)(D + 2);
-                if (c == 0) {
-                    p[0] = M;
-                    p[1] = Ls;
-                }
-                p[2 + c] = O;
-            }
-        }
+        if (!whole && kg == 0 && n16 < G) *reinterpret_cast<float2 *>(st + n16 * (D + 2)) = make_float2(m, l);
         if constexpr (SHARED) {
-            if (tid == 0) {
-                if (tile == 0) a.spans[unit].x = blockIdx.x;
-                if (tend == tiles) a.spans[unit].y = blockIdx.x;
+            if (lane == 0) {
+                if (begun == 0) a.spans[unit].x = blockIdx.x;
+                if (last) a.spans[unit].y = blockIdx.x;
             }
-            __syncthreads();                 // the states have been read
+        }
+    };
+
+    begin_unit(cur.unit);
+    if (cur.left == 0) {                     // a whole unit without rows
+        end_unit(cur.unit, true);
+        return;
+    }
+    Cursor4 rows = cur, ents = cur;
+    const int steps = cur.left;
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) {
+        issue_entries(ents, s);
+        advance(ents);
+    }
+    wait_vmem<0>();
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) {
+        issue_rows(rows, s);
+        advance(rows);
+        issue_entries(ents, (s + NS - 1) % NS);
+        advance(ents);
+    }
+    for (int st = 0; st < steps; ++st) {
+        // the rows of this step and the entries of the rows issued below; what
+        // else has been issued since (logits, states) only makes this stricter
+        wait_vmem<(NS - 2) * L::LOADS>();
+        issue_rows(rows, (st + NS - 1) % NS);
+        advance(rows);
+        issue_entries(ents, (st + NS - 2) % NS);
+        advance(ents);
+        const int slot = st % NS;
+                        const char *sb = ring + slot * L::SLOT;
+                        const uint8_t *sc = reinterpret_cast<const uint8_t *>(sb + 2 * L::CODES);
+                        const uint32_t live = (uint32_t)__ballot((valid >> slot) & 1u);      // bit i: row i of the tile counts
+                        // logits: lane (n16, kg) of half u gets rows 16 u + 4 kg + i of head n16
+                        float z[8];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int row = 16 * u + n16;
+                            uint32_t kw[STEPS];
+                            uint32_t byte;
+                            if constexpr (D == 128) {
+                                const v4u x = *reinterpret_cast<const v4u *>(sb + row * 64 + ((kg ^ (n16 / 4)) * 16));
+#pragma unroll
+                                for (int s = 0; s < STEPS; ++s) kw[s] = x[s];
+                                byte = sc[row * SB + kg];
+                            } else {
+                                const uint2 x = *reinterpret_cast<const uint2 *>(sb + row * 32 + kg * 8);
+                                kw[0] = x.x;
+                                kw[1] = x.y;
+                                byte = sc[row * SB + kg / 2];
+                            }
+                            const float ks = fp4_scale(byte);
+                            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int s = 0; s < STEPS; ++s) {
+                                const bf16x8 kf = as_bf16x8(v4u{fp4_bf16_pair<0>(kw[s], ks), fp4_bf16_pair<1>(kw[s], ks),
+                                                                fp4_bf16_pair<2>(kw[s], ks), fp4_bf16_pair<3>(kw[s], ks)});
+#pragma unroll
+                                for (int p = 0; p < PARTS; ++p)
+                                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][s], acc, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i] * a.scale_log2;
+                        }
+                        if (live != 0xffffffffu) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                z[i] = (live >> (16 * (i / 4) + 4 * kg + i % 4)) & 1u ? z[i] : -INFINITY;
+                        }
+                        if constexpr (KEEP) {
+                            if (n16 < G) {
+                                float *zp = a.z + ((int64_t)cur.unit * G + n16) * a.z_stride + (int64_t)cur.tile * D4_TILE + 4 * kg;
+#pragma unroll
+                                for (int u = 0; u < 2; ++u)
+                                    *reinterpret_cast<float4 *>(zp + 16 * u) =
+                                        make_float4(z[4 * u], z[4 * u + 1], z[4 * u + 2], z[4 * u + 3]);
+                            }
+                        }
+                        float top = z[0];
+#pragma unroll
+                        for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+                        if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
+                            top = fmaxf(top, __shfl_xor(top, 16, 64));
+                            top = fmaxf(top, __shfl_xor(top, 32, 64));
+                            const float mn = fmaxf(m, top);
+                            const float f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                            l *= f;
+                            m = mn;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float fi = __shfl(f, 4 * kg + i, 64);
+#pragma unroll
+                                for (int j = 0; j < NC; ++j) o[j][i] *= fi;
+                            }
+                        }
+                        const float ref = m == -INFINITY ? 0.f : m;
+                        uint32_t pw[3][8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float p = __builtin_amdgcn_exp2f(z[i] - ref);
+                            l += p;
+                            uint32_t x[3];
+                            split3(p, x);
+#pragma unroll
+                            for (int k = 0; k < 3; ++k) pw[k][i] = x[k];
+                        }
+                        bf16x8 pf[3];
+#pragma unroll
+                        for (int k = 0; k < 3; ++k)
+                            pf[k] = as_bf16x8(v4u{high_halves(pw[k][0], pw[k][1]), high_halves(pw[k][2], pw[k][3]),
+                                                  high_halves(pw[k][4], pw[k][5]), high_halves(pw[k][6], pw[k][7])});
+                        // values: 8 rows x NC channels per lane, as bf16 pairs of channels, then of rows
+                        uint32_t vb[8][NC / 2];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int place = 16 * (i / 4) + 4 * (i % 4) + kg, row = 16 * (i / 4) + 4 * kg + i % 4;
+                            const char *vp = sb + L::CODES + place * (D / 2);
+                            uint32_t byte = sc[row * SB + SB / 2 + n16 * NC / FP4_BLOCK];
+                            // a row that is left out stands on pool row 0: its zero
+                            // probability must not meet a NaN
+                            if (live != 0xffffffffu) byte = (live >> row) & 1u ? byte : 0u;
+                            const float vs = fp4_scale(byte);
+                            uint32_t w;
+                            if constexpr (NC == 8) w = *reinterpret_cast<const uint32_t *>(vp + n16 * 4);
+                            else w = *reinterpret_cast<const uint16_t *>(vp + n16 * 2);
+                            vb[i][0] = fp4_bf16_pair<0>(w, vs);
+                            vb[i][1] = fp4_bf16_pair<1>(w, vs);
+                            if constexpr (NC == 8) {
+                                vb[i][2] = fp4_bf16_pair<2>(w, vs);
+                                vb[i][3] = fp4_bf16_pair<3>(w, vs);
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < NC; ++j) {
+                            v4u w;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                w[i] = __builtin_amdgcn_perm(vb[2 * i + 1][j / 2], vb[2 * i][j / 2],
+                                                             j % 2 == 0 ? 0x05040100u : 0x07060302u);
+                            const bf16x8 vf = as_bf16x8(w);
+#pragma unroll
+                            for (int k = 0; k < 3; ++k)
+                                o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[k], vf, o[j], 0, 0, 0);
+                        }
+        const int unit = cur.unit;
+        const bool last = (cur.tile + 1) * D4_TILE >= cur.n;
+        advance(cur);
+        if (last || cur.left <= 0) {
+            end_unit(unit, last);
+            if (cur.left > 0) {
+                begun = 0;
+                begin_unit(cur.unit);
+            }
         }
     }
+    wait_vmem<0>();                          // nothing is under way to the LDS of whoever runs here next
 }
 
-// Whether workgroups share the tiles of all units: where a unit could be cut
-// and the units are not so many that whole ones keep the chip even (eight per
-// CU).
+// Whether wavefronts share the tiles of all units: where a unit could be cut,
+// and the units are not too many for the lookup (64 per lane; the chip holds
+// 2,048 wavefronts).
 static bool shares_tiles(int64_t units, int64_t max_rows) {
-    return max_rows > D4_WAVES * D4_TILE && units <= D4_SHARED_UNITS;
+    return max_rows > D4_MIN_SHARE * D4_TILE && units <= D4_SHARED_UNITS;
 }
-// Workgroups that share them (the kernel uses fewer where the units are short).
-static int64_t shared_wgs(int64_t units, int64_t max_rows) {
-    return std::max<int64_t>(1, std::min<int64_t>(D4_WGS, units * ceil_div(max_rows, D4_TILE) / D4_WAVES));
+// Wavefronts that share them (the kernel uses fewer where the units are short).
+static int64_t shared_waves(int64_t units, int64_t max_rows) {
+    return std::max<int64_t>(1, std::min<int64_t>(D4_SHARES, units * ceil_div(max_rows, D4_TILE) / D4_MIN_SHARE));
 }
 
 struct Decode4Sizes {      // bytes of the workspace's parts
@@ -457,7 +480,7 @@ struct Decode4Sizes {      // bytes of the workspace's parts
 };
 static Decode4Sizes decode4_sizes(int64_t units, int G, int d, int64_t max_rows, bool weights) {
     const bool shared = shares_tiles(units, max_rows);
-    const size_t slots = shared ? (size_t)(units + shared_wgs(units, max_rows)) : weights ? (size_t)units : 0;
+    const size_t slots = shared ? (size_t)(units + shared_waves(units, max_rows)) : weights ? (size_t)units : 0;
     return {weights ? (size_t)units * G * z_stride_of(max_rows) * sizeof(float) : 0,
             slots * G * (size_t)(d + 2) * sizeof(float), shared ? (size_t)units * sizeof(int2) : 0};
 }
@@ -476,17 +499,16 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     a.z_stride = w.z_stride = z_stride_of(max_rows);
     a.spans = shared ? reinterpret_cast<int2 *>(ws + sz.z) : nullptr;
     a.states = reinterpret_cast<float *>(ws + sz.z + sz.spans);
-    const unsigned grid = shared ? (unsigned)shared_wgs(units, max_rows) : (unsigned)units;
-#define SG_D4(KEEP, SHARED) decode4_kernel<T, D, KEEP, SHARED><<<grid, D4_THREADS, 0, s>>>(a)
+    const unsigned grid = shared ? (unsigned)shared_waves(units, max_rows) : (unsigned)units;
+#define SG_D4(KEEP, SHARED) decode4_kernel<T, D, KEEP, SHARED><<<grid, 64, 0, s>>>(a)
     if (weights && shared) SG_D4(true, true);
     else if (weights) SG_D4(true, false);
     else if (shared) SG_D4(false, true);
     else SG_D4(false, false);
 #undef SG_D4
     if (weights || shared) {
-        const dim3 fgrid((unsigned)units, weights ? (unsigned)ceil_div(max_rows, FINISH_ROWS) : 1u);
-        decode_finish_kernel<D><<<fgrid, FINISH_THREADS, 0, s>>>(a.Hq, a.Hkv, 1, a.n_rows, max_rows, 0, a.spans,
-                                                                 a.states, a.out, w);
+        decode_finish_kernel<D><<<finish_grid<D>(units, G, weights, max_rows), FINISH_THREADS, 0, s>>>(
+            G, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
     }
     return launch_status(fn);
 }
@@ -517,7 +539,7 @@ extern "C" int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int 
     SG_REQUIRE((int64_t)max_pages * page_size <= (1ll << 30), SG_EINVAL, "%s: page table too large", fn);
     SG_REQUIRE(pool_rows <= 0x7fffffffll, SG_EUNSUPPORTED, "%s: pool above 2^31 rows", fn);
     SG_REQUIRE(scale > 0.f && scale <= 3.4e38f, SG_EINVAL, "%s: scale must be positive and finite", fn);
-    SG_REQUIRE((int64_t)B * Hkv <= max_workgroups(D4_THREADS), SG_EUNSUPPORTED, "%s: too many units", fn);
+    SG_REQUIRE((int64_t)B * Hkv <= max_workgroups(64), SG_EUNSUPPORTED, "%s: too many units", fn);
     if (weight_out) {
         SG_REQUIRE(weight_stride >= (int64_t)max_pages * page_size, SG_EINVAL, "%s: weight rows of %lld floats hold no %lld rows",
                    fn, (long long)weight_stride, (long long)max_pages * page_size);
@@ -534,6 +556,9 @@ extern "C" int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int 
     while ((1ll << lg) < page_size) ++lg;
     const int shift = 30 + lg;
     const uint32_t mul = (uint32_t)(((1ull << shift) + (uint64_t)page_size - 1) / (uint64_t)page_size);
+    // rows that are left out read pool row 0 and nothing comes of it: where the
+    // pool has no rows, the queries (a row of them is longer) stand for it
+    if (pool_rows == 0) k_pool = v_pool = s_pool = reinterpret_cast<const uint8_t *>(q);
     const Decode4Args a{Hq, Hkv, scale * 1.4426950408889634f /* log2(e) */, q, k_pool, v_pool, s_pool, pool_rows,
                         page_table, n_rows, page_size, max_pages, 0, mul, shift, out, nullptr, nullptr, nullptr, 0};
     hipStream_t s = as_stream(stream);

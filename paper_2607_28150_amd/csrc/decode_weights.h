@@ -40,70 +40,124 @@ __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_
     return split_rows > 0 ? (int)min<int64_t>(nsplit, ceil_div(n, split_rows)) : (n > 0 ? nsplit : 0);
 }
 
-// Grid: x = unit, y = chunk of FINISH_ROWS rows (chunk 0 also writes the
-// unit's outputs).  States of a unit: nsplit places, of which the used ones come
-// first; or, with `spans`, places unit + spans[unit].x .. unit + spans[unit].y,
-// where a unit with one state and no weights has its output already.
+// Grid: x = unit; y below merge_blocks(G): FINISH_THREADS / D heads' outputs,
+// then chunks of FINISH_ROWS rows' weights.  States of a unit: nsplit places, of
+// which the used ones come first; or, with `spans`, places unit +
+// spans[unit].x .. unit + spans[unit].y, where a unit with one state and no
+// weights has its output already.
+//
+// Latency alone for small calls: the loads of a step are issued together (row
+// count and span, then eight states; for the weights the rows' logits of four
+// heads), so either kind of block takes three round trips.
+template <int D>
+constexpr int merge_blocks(int G) { return (G * D + FINISH_THREADS - 1) / FINISH_THREADS; }
+
+template <int D>
+static dim3 finish_grid(int64_t units, int G, bool weights, int64_t max_rows) {
+    return dim3((unsigned)units,
+                (unsigned)(merge_blocks<D>(G) + (weights ? ceil_div(max_rows, FINISH_ROWS) : 0)));
+}
+
 template <int D>
 static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
-    int Hq, int Hkv, int nsplit, const int32_t *__restrict__ n_rows, int64_t max_rows, int64_t split_rows,
+    int G, int nsplit, const int32_t *__restrict__ n_rows, int64_t max_rows, int64_t split_rows,
     const int2 *__restrict__ spans, const float *__restrict__ states, float *__restrict__ out, Weights w) {
-    __shared__ float M[FINISH_MAX_G], inv[FINISH_MAX_G];
-    const int G = Hq / Hkv;
+    constexpr int GROUP = 8;       // states whose loads are in flight together
     const int64_t unit = blockIdx.x;
+    const int2 sp = spans ? spans[unit] : make_int2(0, 0);
     const int64_t n = max<int64_t>(0, min<int64_t>(n_rows[unit], max_rows));
-    if (blockIdx.y > 0 && (int64_t)blockIdx.y * FINISH_ROWS >= n) return;      // uniform
+    const int chunk = (int)blockIdx.y - merge_blocks<D>(G);
+    if (chunk >= 0 && (int64_t)chunk * FINISH_ROWS >= n) return;       // uniform
     int used = used_splits(n, nsplit, split_rows);
     int64_t first = unit * nsplit;
     if (spans && n > 0) {
-        const int2 sp = spans[unit];
         if (sp.x == sp.y && !w.out) return;      // uniform
         used = sp.y - sp.x + 1;
         first = unit + sp.x;
     }
     const float *st = states + first * G * (int64_t)(D + 2);
+    const int64_t step = (int64_t)G * (D + 2);
+
+    if (chunk < 0) {
+        const int g = (int)blockIdx.y * (FINISH_THREADS / D) + threadIdx.x / D, c = threadIdx.x % D;
+        if (g >= G) return;
+        const float *p = st + (int64_t)g * (D + 2);
+        float M = -INFINITY, L = 0.f, O = 0.f;
+        for (int s0 = 0; s0 < used; s0 += GROUP) {
+            float m[GROUP], l[GROUP], o[GROUP];
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) {
+                const float *x = p + min(s0 + j, used - 1) * step;
+                m[j] = x[0];
+                l[j] = x[1];
+                o[j] = x[2 + c];
+            }
+            float top = M;
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) top = fmaxf(top, m[j]);        // (past the last: it again)
+            const float f = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
+            L *= f;
+            O *= f;
+            M = top;
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j)
+                if (s0 + j < used) {
+                    const float a = m[j] == M ? 1.f : __builtin_amdgcn_exp2f(m[j] - M);
+                    L += a * l[j];
+                    O += a * o[j];
+                }
+        }
+        out[(unit * G + g) * D + c] = L == 0.f ? 0.f : O / L;
+        return;
+    }
+
+    __shared__ float M_s[FINISH_MAX_G], inv_s[FINISH_MAX_G];
     const int lane = threadIdx.x % 64;
     for (int g = threadIdx.x / 64; g < G; g += FINISH_THREADS / 64) {
-        float m = -INFINITY, l = 0.f;
-        for (int s = lane; s < used; s += 64) m = fmaxf(m, st[((int64_t)s * G + g) * (D + 2)]);
-        m = wave_max(m);
-        for (int s = lane; s < used; s += 64) {
-            const float *p = st + ((int64_t)s * G + g) * (D + 2);
-            l += p[1] * (p[0] == m ? 1.f : __builtin_amdgcn_exp2f(p[0] - m));
+        const float *p = st + (int64_t)g * (D + 2);
+        float M = -INFINITY, L = 0.f;
+        for (int s0 = 0; s0 < used; s0 += 64) {
+            const bool in = s0 + lane < used;
+            const float *x = p + min(s0 + lane, used - 1) * step;
+            const float m = x[0], l = x[1];
+            const float top = fmaxf(M, wave_max(m));
+            const float a = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            const float sum = wave_sum(in ? a * l : 0.f);
+            L = L * (M == top ? 1.f : __builtin_amdgcn_exp2f(M - top)) + sum;
+            M = top;
         }
-        l = wave_sum(l);
         if (lane == 0) {
-            M[g] = m;
-            inv[g] = l == 0.f ? 0.f : 1.f / l;
+            M_s[g] = M == -INFINITY ? 0.f : M;
+            inv_s[g] = L == 0.f ? 0.f : 1.f / L;
         }
     }
     __syncthreads();
-    if (blockIdx.y == 0) {
-        const int b = (int)(unit / Hkv), h = (int)(unit % Hkv);
-        for (int i = threadIdx.x; i < G * D; i += FINISH_THREADS) {
-            const int g = i / D, c = i % D;
-            float o = 0.f;
-            for (int s = 0; s < used; ++s) {
-                const float *p = st + ((int64_t)s * G + g) * (D + 2);
-                o += p[2 + c] * (p[0] == M[g] ? 1.f : __builtin_amdgcn_exp2f(p[0] - M[g]));
+    // four rows per thread, four heads at a time (rows past n lie within the
+    // unit's logits, or are not read)
+    const int64_t i = (int64_t)chunk * FINISH_ROWS + threadIdx.x * 4;
+    if (i >= n) return;
+    float add[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
+    const int64_t at = unit * w.stride + i;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) old[j] = w.in && i + j < n ? w.in[at + j] : 0.f;
+    for (int g0 = 0; g0 < G; g0 += 4) {
+        float4 z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            z[k] = *reinterpret_cast<const float4 *>(w.z + (unit * G + min(g0 + k, G - 1)) * w.z_stride + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (g0 + k < G && inv_s[g0 + k] != 0.f) {      // (an empty pool leaves z unwritten)
+                const float M = M_s[g0 + k], f = inv_s[g0 + k];
+                add[0] += __builtin_amdgcn_exp2f(z[k].x - M) * f;
+                add[1] += __builtin_amdgcn_exp2f(z[k].y - M) * f;
+                add[2] += __builtin_amdgcn_exp2f(z[k].z - M) * f;
+                add[3] += __builtin_amdgcn_exp2f(z[k].w - M) * f;
             }
-            out[((int64_t)b * Hq + (int64_t)h * G + g) * D + c] = o * inv[g];
-        }
     }
-    if (!w.out) return;
-    const int64_t i0 = (int64_t)blockIdx.y * FINISH_ROWS + threadIdx.x;
-    for (int j = 0; j < 4; ++j) {
-        const int64_t i = i0 + j * FINISH_THREADS;
-        if (i >= n) break;
-        float p = 0.f;
-        for (int g = 0; g < G; ++g) {
-            const float z = w.z[(unit * G + g) * w.z_stride + i];
-            const float e = __builtin_amdgcn_exp2f(z - (M[g] == -INFINITY ? 0.f : M[g]));
-            p += inv[g] == 0.f ? 0.f : e * inv[g];     // (an empty pool leaves z unwritten)
-        }
-        const float old = w.in ? w.decay * w.in[unit * w.stride + i] : 0.f;
-        w.out[unit * w.stride + i] = old + p;
-    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n) w.out[at + j] = w.decay * old[j] + add[j];
 }
 
 }  // namespace sg
