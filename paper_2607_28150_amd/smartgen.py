@@ -567,25 +567,53 @@ def sg_spec_commit(ids, L, Hkv, T, s0, N, M, mask, rem=None, stream=None):
 
 # ----------------------------------------------------------------------------- 4-bit rows
 
-def _here(*tensors):
-    """Device tensors of one call lie on the current device, where its kernels run."""
-    now = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+def _addresses(*tensors):
+    """Device-usable addresses of one call's tensors (see _ptr); those in device
+    memory lie on the current device, where the call's kernels run."""
+    device, out = -1, []
     for t in tensors:
-        _need(t is None or not t.is_cuda or t.device.index == now,
-              f"a tensor lies on {None if t is None else t.device}, the current device is {now}")
+        if t is None:
+            out.append(None)
+        elif t.is_cuda:
+            if not t.is_contiguous():
+                raise ValueError("tensors passed to the library must be contiguous")
+            if t.get_device() != device:
+                device = torch.cuda.current_device()
+                if t.get_device() != device:
+                    raise ValueError(f"a tensor lies on {t.device}, the current device is {device}")
+            out.append(t.data_ptr())
+        else:
+            out.append(_ptr(t))
+    return out
+
+
+def _stream_address(stream):
+    """The raw stream of a call (torch's current one without building its object)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _bytes_of(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
 
 
 def _row_code(k, v, s, d, what):
     """Element type of K/V rows of d channels: uint8 codes with their scales, or f32 / bf16 without."""
-    _need(k.dtype == v.dtype, f"the K and V {what} differ in type")
+    if k.dtype != v.dtype:
+        raise ValueError(f"the K and V {what} differ in type")
     if k.dtype != torch.uint8:
-        _need(s is None, f"{what}: scales go with uint8 codes only")
-        _need(v.numel() >= k.numel() // d * d, f"the V {what} is smaller than the K {what}")
-        return _dtype_code(k), k.numel() // d
+        if s is not None:
+            raise ValueError(f"{what}: scales go with uint8 codes only")
+        rows = k.numel() // d
+        if v.numel() < rows * d:
+            raise ValueError(f"the V {what} is smaller than the K {what}")
+        return _dtype_code(k), rows
     rows = k.numel() // (d // 2)
-    _need(s is not None and s.dtype == torch.uint8, f"{what}: uint8 codes need uint8 scales [rows][2][d / 32]")
-    _need(v.numel() >= rows * (d // 2) and s.numel() >= rows * (d // 16),
-          f"the V codes or scales of the {what} are smaller than its K codes")
+    if s is None or s.dtype != torch.uint8:
+        raise ValueError(f"{what}: uint8 codes need uint8 scales [rows][2][d / 32]")
+    if v.numel() < rows * (d // 2) or s.numel() < rows * (d // 16):
+        raise ValueError(f"the V codes or scales of the {what} are smaller than its K codes")
     return SG_FP4, rows
 
 
@@ -594,7 +622,8 @@ def _row_width(k):
 
 
 def _int32(t, n, what):
-    _need(t.dtype == torch.int32 and t.numel() >= n, f"{what} must be int32 with {n} entries")
+    if t.dtype != torch.int32 or t.numel() < n:
+        raise ValueError(f"{what} must be int32 with {n} entries")
 
 
 def sg_fetch_fp4(row_off, total, index, n_valid, src_row_base, k_src, v_src, page_table, page_size, dst_start,
@@ -616,11 +645,11 @@ def sg_fetch_fp4(row_off, total, index, n_valid, src_row_base, k_src, v_src, pag
         _int32(n_valid, rows, "n_valid")
     if index is not None:
         _int32(index, total, "index")
-    _here(row_off, index, n_valid, src_row_base, k_src, v_src, s_src, page_table, dst_start, k_pool, v_pool, s_pool)
-    rc = load().sg_fetch_fp4(_stream(stream), src_dt, dst_dt, d, rows, _ptr(row_off), int(total), _ptr(index),
-                             _ptr(n_valid), _ptr(src_row_base), src_rows, _ptr(k_src), _ptr(v_src), _ptr(s_src),
-                             _ptr(page_table), int(page_size), int(max_pages), _ptr(dst_start), _ptr(k_pool),
-                             _ptr(v_pool), _ptr(s_pool), pool_rows)
+    (p_off, p_index, p_valid, p_base, p_k, p_v, p_s, p_table, p_start, p_kp, p_vp, p_sp) = _addresses(
+        row_off, index, n_valid, src_row_base, k_src, v_src, s_src, page_table, dst_start, k_pool, v_pool, s_pool)
+    rc = load().sg_fetch_fp4(_stream_address(stream), src_dt, dst_dt, d, rows, p_off, int(total), p_index, p_valid,
+                             p_base, src_rows, p_k, p_v, p_s, p_table, int(page_size), max_pages, p_start, p_kp, p_vp,
+                             p_sp, pool_rows)
     _check("sg_fetch_fp4", rc)
 
 
@@ -661,12 +690,12 @@ def sg_decode_attn_acc(q, k_pool, v_pool, page_table, n_rows, page_size, out, we
     _need(k_pool.dtype == q.dtype and v_pool.dtype == q.dtype, "q and pools must share a dtype")
     pool_rows = k_pool.numel() // d
     _need(v_pool.numel() >= pool_rows * d, "v_pool smaller than k_pool")
-    _here(q, k_pool, v_pool, page_table, n_rows, out, weight, weight_out, ws)
-    rc = load().sg_decode_attn_acc(_stream(stream), _dtype_code(q), B, Hq, Hkv, d,
-                                   float(d ** -0.5 if scale is None else scale), _ptr(q), _ptr(k_pool), _ptr(v_pool),
-                                   pool_rows, _ptr(page_table), _ptr(n_rows), int(page_size), max_pages, _ptr(out),
-                                   _ptr(weight), float(decay), _ptr(weight_out), stride, _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size())
+    p_q, p_k, p_v, p_table, p_n, p_out, p_in, p_w, p_ws = _addresses(q, k_pool, v_pool, page_table, n_rows, out, weight,
+                                                                     weight_out, ws)
+    rc = load().sg_decode_attn_acc(_stream_address(stream), _dtype_code(q), B, Hq, Hkv, d,
+                                   d ** -0.5 if scale is None else float(scale), p_q, p_k, p_v, pool_rows, p_table, p_n,
+                                   int(page_size), max_pages, p_out, p_in, float(decay), p_w, stride, p_ws,
+                                   _bytes_of(ws))
     _check("sg_decode_attn_acc", rc)
     return out
 
@@ -679,12 +708,12 @@ def sg_decode_attn_fp4(q, k_pool, v_pool, s_pool, page_table, n_rows, page_size,
     B, Hq, Hkv, d, max_pages, stride = _decode_shape(q, page_table, n_rows, out, page_size, weight, weight_out)
     code, pool_rows = _row_code(k_pool, v_pool, s_pool, d, "pool")
     _need(code == SG_FP4 and _row_width(k_pool) == d, "the pools must be uint8 codes [rows][d / 2]")
-    _here(q, k_pool, v_pool, s_pool, page_table, n_rows, out, weight, weight_out, ws)
-    rc = load().sg_decode_attn_fp4(_stream(stream), _dtype_code(q), B, Hq, Hkv, d,
-                                   float(d ** -0.5 if scale is None else scale), _ptr(q), _ptr(k_pool), _ptr(v_pool),
-                                   _ptr(s_pool), pool_rows, _ptr(page_table), _ptr(n_rows), int(page_size), max_pages,
-                                   _ptr(out), _ptr(weight), float(decay), _ptr(weight_out), stride, _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size())
+    p_q, p_k, p_v, p_s, p_table, p_n, p_out, p_in, p_w, p_ws = _addresses(q, k_pool, v_pool, s_pool, page_table, n_rows,
+                                                                          out, weight, weight_out, ws)
+    rc = load().sg_decode_attn_fp4(_stream_address(stream), _dtype_code(q), B, Hq, Hkv, d,
+                                   d ** -0.5 if scale is None else float(scale), p_q, p_k, p_v, p_s, pool_rows, p_table,
+                                   p_n, int(page_size), max_pages, p_out, p_in, float(decay), p_w, stride, p_ws,
+                                   _bytes_of(ws))
     _check("sg_decode_attn_fp4", rc)
     return out
 
@@ -717,10 +746,10 @@ def sg_evict(k_pool, v_pool, page_table, n_rows, page_size, budget, weight, n_ke
     for p in (pos, pos_out):
         _need(p is None or (p.dtype == torch.int32 and p.shape[-1] == stride and p.numel() >= units * stride),
               "pos and pos_out must be int32 like weight")
-    _here(k_pool, v_pool, s_pool, page_table, n_rows, budget, weight, pos, recent_from, n_kept, weight_out, pos_out, ws)
-    rc = load().sg_evict(_stream(stream), dt, units, d, _ptr(k_pool), _ptr(v_pool), _ptr(s_pool), pool_rows,
-                         _ptr(page_table), _ptr(n_rows), int(page_size), max_pages, _ptr(budget), _ptr(weight),
-                         _ptr(pos), stride, int(sinks), _ptr(recent_from), _ptr(n_kept), _ptr(weight_out),
-                         _ptr(pos_out), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    (p_k, p_v, p_s, p_table, p_n, p_budget, p_w, p_pos, p_recent, p_kept, p_wout, p_pout, p_ws) = _addresses(
+        k_pool, v_pool, s_pool, page_table, n_rows, budget, weight, pos, recent_from, n_kept, weight_out, pos_out, ws)
+    rc = load().sg_evict(_stream_address(stream), dt, units, d, p_k, p_v, p_s, pool_rows, p_table, p_n, int(page_size),
+                         max_pages, p_budget, p_w, p_pos, stride, int(sinks), p_recent, p_kept, p_wout, p_pout, p_ws,
+                         _bytes_of(ws))
     _check("sg_evict", rc)
     return n_kept
