@@ -1,152 +1,243 @@
 // sg_evict: cuts paged sets to a budget by accumulated weight.
 //
 // Select: one workgroup of 1024 threads per unit ranks the unit's rows like
-// sg_topk (select_common.h; guarded rows carry the highest key of all) into an
-// ascending list of the k kept rows.  The list splits at row k: its first c
-// entries stay where they are, the other k - c move, and they fill the k - c
-// rows below k that are missing from the first part.  Hole i is i + j for the
-// smallest j with list[j] - j > i (list[j] - j rows are missing before list[j],
-// a non-decreasing count), one binary search per hole.  Sources lie at or past
-// k and destinations below it, so the moves need no order among themselves.
+// sg_topk (select_common.h; guarded rows carry the highest key of all) into a
+// bit per row in LDS, with the number of kept rows before every 32.  A row's
+// rank among the kept ones is then two LDS reads: the i-th row below k that is
+// not kept is the i-th hole, the i-th kept row at or past k moves into it, and
+// both write their half of the unit's i-th move.  Sources lie at or past k and
+// destinations below it, so the moves need no order among themselves.
 //
-// Move: K and V rows (and scales) of the listed moves, 16 bytes per lane.
+// Move: K and V rows (and scales), weights and positions of the listed moves,
+// 16 bytes per lane: in the same launch, by the unit's own workgroup, where the
+// units give every CU one; else in a second launch with many workgroups per
+// unit.
 #include "select_common.h"
 
 namespace sg {
 
 constexpr int MOVE_THREADS = 256;
-constexpr int MOVE_UNROLL = 4;
+constexpr int MOVE_UNROLL = 4;      // moves per lane group in flight, in a launch of their own
 
 // Key of a guarded row: above that of every weight (+inf has 0xff800000), and
 // not the largest word (the select looks at keys above its threshold).
 constexpr uint32_t GUARD_KEY = 0xff800001u;
 
-constexpr int evict_waves(int items) { return items <= 32 ? 8 : 4; }
+// Two workgroups per CU while a row's keys fit.
+constexpr int evict_waves(int items) { return items <= 16 ? 8 : 4; }
 
-// Workspace: int2 moves [units][cap / 2] (pool rows: to, from), int32 list
-// [units][cap], int32 counts [units].
-template <int ITEMS>
-__global__ __launch_bounds__(TOPK_THREADS) __attribute__((amdgpu_waves_per_eu(evict_waves(ITEMS)))) void evict_select_kernel(
-    int64_t pool_rows, const int32_t *__restrict__ page_table, const int32_t *n_rows, int page_size, int max_pages,
-    const int32_t *__restrict__ budget, const float *weight, const int32_t *pos, int64_t stride, int sinks,
-    const int32_t *__restrict__ recent_from, int32_t *n_kept, float *weight_out, int32_t *pos_out,
-    int2 *__restrict__ moves, int32_t *list_all, int32_t *__restrict__ counts) {
-    __shared__ SelectSmem sm;
-    const int64_t unit = blockIdx.x;
-    const int tid = threadIdx.x, cap = max_pages * page_size;
-    const int n = min(max((int)n_rows[unit], 0), cap);
-    const int k = min(max((int)budget[unit], 0), n);
-    const float *w = weight + unit * stride;
-    const int32_t *ps = pos ? pos + unit * stride : nullptr;
-    float *wo = weight_out + unit * stride;
-    int32_t *po = pos_out ? pos_out + unit * stride : nullptr;
-    int32_t *list = list_all + unit * cap;
-    const int32_t *pt = page_table + unit * max_pages;
-    int c = k, m = 0;           // kept rows that stay, that move
-    if (k > 0 && k < n) {
-        const int32_t recent = recent_from ? recent_from[unit] : 0x7fffffff;
-        const int it = select_items(n), entry0 = select_entry(it);
-        uint32_t key[ITEMS];
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            key[i] = 0u;
-            if (i < it) {
-                const int row = entry0 + i * 64, at = min(row, n - 1);
-                const float x = w[at];
-                const int32_t p = ps ? ps[at] : at;
-                const bool guard = p < sinks || (recent_from && p >= recent);
-                if (row < n) key[i] = guard ? GUARD_KEY : order_key(x);
-            }
-        }
-        select_top<ITEMS>(key, it, k, list, sm);
-        __syncthreads();        // the list is read by other threads than wrote it
-        int lo = 0, hi = k;     // entries below k
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (list[mid] < k) lo = mid + 1;
-            else hi = mid;
-        }
-        c = lo;
-        m = k - c;
-    }
-    for (int i = tid; i < c; i += TOPK_THREADS) {
-        const int row = k < n ? list[i] : i;
-        if (wo != w) wo[row] = w[row];
-        if (po && po != ps) po[row] = ps[row];
-    }
+struct EvictArgs {
+    v4u *k_pool, *v_pool;
+    uint8_t *s_pool;
+    int64_t pool_rows;
+    const int32_t *page_table, *n_rows;
+    int page_size, max_pages;
+    const int32_t *budget;
+    const float *weight;            // (outputs may be their inputs: no restrict)
+    const int32_t *pos;
+    int64_t stride;
+    int sinks;
+    const int32_t *recent_from;
+    int32_t *n_kept;
+    float *weight_out;
+    int32_t *pos_out;
+    int2 *moves;                    // [units][cap / 2]: rows of the unit, to and from
+    int32_t *counts;                // [units]
+};
+
+// Carries out moves first, first + step, ... of a unit's m, whole groups of
+// CPR lanes (16-byte vectors per K or V row) at a time; SB: bytes of a row's
+// scales.
+template <int CPR, int SB, int UNROLL>
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int64_t unit, int m, int first, int step, int c) {
+    const int2 *mv = a.moves + unit * (a.max_pages * a.page_size / 2);
+    const int32_t *pt = a.page_table + unit * a.max_pages;
+    const float *w = a.weight + unit * a.stride;
+    const int32_t *ps = a.pos ? a.pos + unit * a.stride : nullptr;
+    float *wo = a.weight_out + unit * a.stride;
+    int32_t *po = a.pos_out ? a.pos_out + unit * a.stride : nullptr;
     auto pool_row = [&](int row) -> int {
-        const int64_t x = (int64_t)pt[row / page_size] + row % page_size;
-        return x >= 0 && x < pool_rows ? (int)x : -1;
+        const int64_t x = (int64_t)pt[row / a.page_size] + row % a.page_size;
+        return x >= 0 && x < a.pool_rows ? (int)x : -1;
     };
-    for (int i = tid; i < m; i += TOPK_THREADS) {
-        int lo = 0, hi = c;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (list[mid] - mid > i) hi = mid;
-            else lo = mid + 1;
-        }
-        const int to = i + lo, from = list[c + i];
-        const int pr_to = pool_row(to), pr_from = pool_row(from);
-        moves[unit * (cap / 2) + i] = pr_to >= 0 && pr_from >= 0 ? make_int2(pr_to, pr_from) : make_int2(-1, -1);
-        wo[to] = w[from];
-        if (po) po[to] = ps[from];
-    }
-    __syncthreads();            // every weight that moves has been read
-    for (int i = k + tid; i < n; i += TOPK_THREADS) {
-        wo[i] = 0.f;
-        if (po) po[i] = -1;
-    }
-    if (tid == 0) {
-        counts[unit] = m;
-        n_kept[unit] = k;
-    }
-}
-
-// CPR: 16-byte vectors per K (or V) row; SB: bytes of a row's scales.
-template <int CPR, int SB>
-__global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(int cap, const int2 *__restrict__ moves,
-                                                                  const int32_t *__restrict__ counts, v4u *k_pool,
-                                                                  v4u *v_pool, uint8_t *s_pool) {
-    constexpr int EPI = MOVE_THREADS / CPR, EPB = EPI * MOVE_UNROLL;
-    const int64_t unit = blockIdx.x;
-    const int m = counts[unit];
-    const int2 *mv = moves + unit * (cap / 2);
-    const int c = threadIdx.x % CPR, sub = threadIdx.x / CPR;
-    for (int base = blockIdx.y * EPB; base < m; base += (int)gridDim.y * EPB) {
-        int2 e[MOVE_UNROLL];
+    for (int base = first; base < m; base += step * UNROLL) {
+        int2 e[UNROLL];
+        bool in[UNROLL], copy[UNROLL];
+        int to[UNROLL], from[UNROLL];
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j) {
-            const int i = base + sub + j * EPI;
+        for (int j = 0; j < UNROLL; ++j) {
+            const int i = base + j * step;
+            in[j] = i < m;
             e[j] = mv[min(i, m - 1)];
-            if (i >= m) e[j].x = -1;
         }
-        v4u kr[MOVE_UNROLL], vr[MOVE_UNROLL];
-        uint2 sr[MOVE_UNROLL];
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j)
-            if (e[j].x >= 0) {
-                kr[j] = __builtin_nontemporal_load(k_pool + (int64_t)e[j].y * CPR + c);
-                vr[j] = __builtin_nontemporal_load(v_pool + (int64_t)e[j].y * CPR + c);
+        for (int j = 0; j < UNROLL; ++j) {
+            to[j] = pool_row(e[j].x);
+            from[j] = pool_row(e[j].y);
+            copy[j] = in[j] && to[j] >= 0 && from[j] >= 0;
+        }
+        v4u kr[UNROLL], vr[UNROLL];
+        uint2 sr[UNROLL];
+        float wr[UNROLL];
+        int32_t pr[UNROLL];
+#pragma unroll
+        for (int j = 0; j < UNROLL; ++j) {
+            if (copy[j]) {
+                kr[j] = __builtin_nontemporal_load(a.k_pool + (int64_t)from[j] * CPR + c);
+                vr[j] = __builtin_nontemporal_load(a.v_pool + (int64_t)from[j] * CPR + c);
+            }
+            if (in[j] && c == 0) {
+                wr[j] = w[e[j].y];
+                if (po) pr[j] = ps[e[j].y];
                 if constexpr (SB > 0)
-                    if (c == 0) {
-                        const uint8_t *p = s_pool + (int64_t)e[j].y * SB;
+                    if (copy[j]) {
+                        const uint8_t *p = a.s_pool + (int64_t)from[j] * SB;
                         if constexpr (SB == 8) sr[j] = *reinterpret_cast<const uint2 *>(p);
                         else sr[j].x = *reinterpret_cast<const uint32_t *>(p);
                     }
             }
+        }
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j)
-            if (e[j].x >= 0) {
-                __builtin_nontemporal_store(kr[j], k_pool + (int64_t)e[j].x * CPR + c);
-                __builtin_nontemporal_store(vr[j], v_pool + (int64_t)e[j].x * CPR + c);
+        for (int j = 0; j < UNROLL; ++j) {
+            if (copy[j]) {
+                __builtin_nontemporal_store(kr[j], a.k_pool + (int64_t)to[j] * CPR + c);
+                __builtin_nontemporal_store(vr[j], a.v_pool + (int64_t)to[j] * CPR + c);
+            }
+            if (in[j] && c == 0) {
+                wo[e[j].x] = wr[j];
+                wo[e[j].y] = 0.f;
+                if (po) {
+                    po[e[j].x] = pr[j];
+                    po[e[j].y] = -1;
+                }
                 if constexpr (SB > 0)
-                    if (c == 0) {
-                        uint8_t *p = s_pool + (int64_t)e[j].x * SB;
+                    if (copy[j]) {
+                        uint8_t *p = a.s_pool + (int64_t)to[j] * SB;
                         if constexpr (SB == 8) *reinterpret_cast<uint2 *>(p) = sr[j];
                         else *reinterpret_cast<uint32_t *>(p) = sr[j].x;
                     }
             }
+        }
     }
+}
+
+// CPR = 0: the moves are left to a second launch.
+template <int ITEMS, int CPR, int SB>
+__global__ __launch_bounds__(TOPK_THREADS) __attribute__((amdgpu_waves_per_eu(evict_waves(ITEMS)))) void evict_select_kernel(
+    EvictArgs a) {
+    __shared__ SelectSmem sm;
+    __shared__ uint32_t kept[ITEMS * 32];        // a bit per row
+    __shared__ int32_t before[ITEMS * 32];       // kept rows before each word
+    const int64_t unit = blockIdx.x;
+    const int tid = threadIdx.x, cap = a.max_pages * a.page_size;
+    const int n = min(max((int)a.n_rows[unit], 0), cap);
+    const int k = min(max((int)a.budget[unit], 0), n);
+    const float *w = a.weight + unit * a.stride;
+    const int32_t *ps = a.pos ? a.pos + unit * a.stride : nullptr;
+    float *wo = a.weight_out + unit * a.stride;
+    int32_t *po = a.pos_out ? a.pos_out + unit * a.stride : nullptr;
+    const bool copy = wo != w || po != ps;       // rows that stay have to be written
+    int m = 0;
+    if (k > 0 && k < n) {
+        const int32_t recent = a.recent_from ? a.recent_from[unit] : 0x7fffffff;
+        const int it = select_items(n), entry0 = select_entry(it);
+        uint32_t key[ITEMS];
+        constexpr int STEP = ITEMS < 8 ? ITEMS : 8;      // rows whose loads are in flight together
+#pragma unroll
+        for (int i0 = 0; i0 < ITEMS; i0 += STEP) {
+#pragma unroll
+            for (int i = i0; i < i0 + STEP; ++i) key[i] = 0u;
+            if (i0 >= it) continue;                      // uniform
+            float x[STEP];
+            int32_t p[STEP];
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const int at = min(entry0 + (i0 + i) * 64, n - 1);
+                x[i] = w[at];
+                p[i] = ps ? ps[at] : at;
+            }
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const bool guard = p[i] < a.sinks || (a.recent_from && p[i] >= recent);
+                if (i0 + i < it && entry0 + (i0 + i) * 64 < n) key[i0 + i] = guard ? GUARD_KEY : order_key(x[i]);
+            }
+        }
+        const int past = (tid / 64 + 1) * 64 * it;       // end of this wavefront's entries
+        select_masks<ITEMS>(key, it, k, sm, [&](int first, uint32_t mask, int p) {
+            if (first < past) {
+                kept[first / 32] = mask;
+                before[first / 32] = p;
+            }
+        });
+        __syncthreads();
+        auto rank = [&](int row) { return before[row / 32] + __popc(kept[row / 32] & ((1u << (row % 32)) - 1u)); };
+        const int c = rank(k);                           // kept rows that stay
+        m = k - c;
+        int2 *mv = a.moves + unit * (cap / 2);
+        for (int i = 0; i < it; ++i) {
+            const int row = entry0 + i * 64;
+            if (row >= n) break;
+            const bool keep = (kept[row / 32] >> (row % 32)) & 1u;
+            const int r = rank(row);
+            if (row < k) {
+                if (!keep) {
+                    mv[row - r].x = row;
+                } else if (copy) {
+                    wo[row] = w[row];
+                    if (po) po[row] = ps[row];
+                }
+            } else if (keep) {
+                mv[r - c].y = row;                       // its weight goes with the move
+            } else {
+                wo[row] = 0.f;
+                if (po) po[row] = -1;
+            }
+        }
+    } else {
+        for (int i = tid; i < n; i += TOPK_THREADS) {
+            if (i >= k) {
+                wo[i] = 0.f;
+                if (po) po[i] = -1;
+            } else if (copy) {
+                wo[i] = w[i];
+                if (po) po[i] = ps[i];
+            }
+        }
+    }
+    __syncthreads();             // every thread has read the row count; the moves are listed
+    if (tid == 0) {
+        if (CPR == 0) a.counts[unit] = m;
+        a.n_kept[unit] = k;
+    }
+    if constexpr (CPR > 0)
+        move_rows<CPR, SB, 1>(a, unit, m, tid / CPR, TOPK_THREADS / CPR, tid % CPR);
+}
+
+template <int CPR, int SB>
+__global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(EvictArgs a) {
+    constexpr int EPI = MOVE_THREADS / CPR, EPB = EPI * MOVE_UNROLL;      // moves per workgroup: one pass
+    const int first = (int)blockIdx.y * EPB, m = min(a.counts[blockIdx.x], first + EPB);
+    move_rows<CPR, SB, MOVE_UNROLL>(a, blockIdx.x, m, first + (int)threadIdx.x / CPR, EPI, threadIdx.x % CPR);
+}
+
+template <int CPR, int SB>
+static int launch_evict(const char *fn, hipStream_t s, int units, const EvictArgs &a) {
+    const int cap = a.max_pages * a.page_size, items = (int)ceil_div(cap, TOPK_THREADS);
+    const bool one = units >= device_cus();
+#define SG_SELECT(I)                                                                                      do {                                                                                                      if (one) evict_select_kernel<I, CPR, SB><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);                 else evict_select_kernel<I, 0, 0><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);                    } while (0)
+    if (items <= 2) SG_SELECT(2);
+    else if (items <= 4) SG_SELECT(4);
+    else if (items <= 8) SG_SELECT(8);
+    else if (items <= 16) SG_SELECT(16);
+    else if (items <= 32) SG_SELECT(32);
+    else if (items <= 64) SG_SELECT(64);
+    else SG_SELECT(80);
+#undef SG_SELECT
+    if (!one) {
+        const dim3 grid((unsigned)units, (unsigned)std::max<int64_t>(1, ceil_div(cap / 2, MOVE_THREADS / CPR * MOVE_UNROLL)));
+        evict_move_kernel<CPR, SB><<<grid, MOVE_THREADS, 0, s>>>(a);
+    }
+    return launch_status(fn);
 }
 
 }  // namespace sg
@@ -156,7 +247,7 @@ using namespace sg;
 extern "C" size_t sg_evict_workspace_size(int units, int max_pages, int page_size) {
     if (units <= 0 || max_pages <= 0 || page_size <= 0) return 0;
     const size_t cap = (size_t)max_pages * page_size;
-    return (size_t)units * (cap / 2 * sizeof(int2) + cap * 4 + 4);
+    return (size_t)units * (cap / 2 * sizeof(int2) + sizeof(int32_t));
 }
 
 extern "C" int sg_evict(void *stream, sg_dtype dt, int units, int d, void *k_pool, void *v_pool, uint8_t *s_pool,
@@ -186,39 +277,16 @@ extern "C" int sg_evict(void *stream, sg_dtype dt, int units, int d, void *k_poo
     const size_t need = sg_evict_workspace_size(units, max_pages, page_size);
     SG_REQUIRE(ws && ws_bytes >= need, SG_EWORKSPACE, "%s: needs %zu bytes of workspace, %zu given", fn, need, ws_bytes);
     int2 *moves = reinterpret_cast<int2 *>(ws);
-    int32_t *list = reinterpret_cast<int32_t *>(moves + (size_t)units * (cap / 2));
-    int32_t *counts = list + (size_t)units * cap;
+    const EvictArgs a{reinterpret_cast<v4u *>(k_pool), reinterpret_cast<v4u *>(v_pool), s_pool, pool_rows, page_table,
+                      n_rows, page_size, max_pages, budget, weight, pos, stride, sinks, recent_from, n_kept, weight_out,
+                      pos_out, moves, reinterpret_cast<int32_t *>(moves + (size_t)units * (cap / 2))};
     hipStream_t s = as_stream(stream);
-    const int items = (int)ceil_div(cap, TOPK_THREADS);
-#define SG_SELECT(I)                                                                                                 \
-    evict_select_kernel<I><<<(unsigned)units, TOPK_THREADS, 0, s>>>(pool_rows, page_table, n_rows, page_size,        \
-                                                                    max_pages, budget, weight, pos, stride, sinks,   \
-                                                                    recent_from, n_kept, weight_out, pos_out, moves, \
-                                                                    list, counts)
-    if (items <= 2) SG_SELECT(2);
-    else if (items <= 4) SG_SELECT(4);
-    else if (items <= 8) SG_SELECT(8);
-    else if (items <= 16) SG_SELECT(16);
-    else if (items <= 32) SG_SELECT(32);
-    else if (items <= 64) SG_SELECT(64);
-    else SG_SELECT(80);
-#undef SG_SELECT
-    const int cpr = dt == SG_FP4 ? d / 32 : d * esize_of(dt) / 16;
-    const int64_t epb = MOVE_THREADS / cpr * MOVE_UNROLL;
-    // about eight workgroups per CU over the units, each unit's moves a grid
-    // stride apart
-    const int64_t ny = std::min(std::max<int64_t>(1, ceil_div(cap / 2, epb)), ceil_div(8 * device_cus(), units));
-    const dim3 grid((unsigned)units, (unsigned)ny);
-    v4u *kp = reinterpret_cast<v4u *>(k_pool), *vp = reinterpret_cast<v4u *>(v_pool);
-#define SG_MOVE(C, SB) evict_move_kernel<C, SB><<<grid, MOVE_THREADS, 0, s>>>(cap, moves, counts, kp, vp, s_pool)
-    switch (cpr) {
-        case 2: SG_MOVE(2, 4); break;
-        case 4: SG_MOVE(4, 8); break;
-        case 8: SG_MOVE(8, 0); break;
-        case 16: SG_MOVE(16, 0); break;
-        case 32: SG_MOVE(32, 0); break;
+    switch (dt == SG_FP4 ? d / 32 : d * esize_of(dt) / 16) {
+        case 2: return launch_evict<2, 4>(fn, s, units, a);
+        case 4: return launch_evict<4, 8>(fn, s, units, a);
+        case 8: return launch_evict<8, 0>(fn, s, units, a);
+        case 16: return launch_evict<16, 0>(fn, s, units, a);
+        case 32: return launch_evict<32, 0>(fn, s, units, a);
         default: set_error("%s: internal row size", fn); return SG_EINTERNAL;
     }
-#undef SG_MOVE
-    return launch_status(fn);
 }

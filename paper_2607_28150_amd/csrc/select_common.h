@@ -111,12 +111,14 @@ __device__ __forceinline__ void select_each(const uint32_t (&key)[ITEMS], int it
     }
 }
 
-// Writes the ids of the kk largest keys (ties: lower id), ascending, to
-// out[0 .. kk).  0 < kk <= number of entries; keys of slots past the row are
-// 0.  Every thread of the workgroup must call it.
-template <int ITEMS>
-__device__ __forceinline__ void select_top(const uint32_t (&key)[ITEMS], int it, int kk, int32_t *out,
-                                           SelectSmem &sm) {
+// Finds the kk largest keys (ties: lower id) and calls emit(first, m, p) for
+// every 32 entries from `first` on: the mask m of those taken, and the number p
+// taken before them.  (Lanes past their wavefront's 64 * it entries call it
+// too, with m = 0.)  0 < kk <= number of entries; keys of slots past the row
+// are 0, and none is 0xffffffff.  Every thread of the workgroup must call it.
+template <int ITEMS, typename Emit>
+__device__ __forceinline__ void select_masks(const uint32_t (&key)[ITEMS], int it, int kk, SelectSmem &sm,
+                                             Emit &&emit) {
     const int tid = threadIdx.x, lane = tid % 64;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
     // loops over the thread's keys stop at the row's own items, four at a time
@@ -313,14 +315,22 @@ __device__ __forceinline__ void select_top(const uint32_t (&key)[ITEMS], int it,
             }
         }
         const int n = __popc(m), sc = wave_scan_incl(n);
-        int p = pos + sc - n;
+        const int p = pos + sc - n;
         pos += __builtin_amdgcn_readlane(sc, 63);
-        const int first = base + (r * HALVES + lane / 2) * 64 + (lane % 2) * 32;
+        emit(base + (r * HALVES + lane / 2) * 64 + (lane % 2) * 32, m, p);
+    }
+}
+
+// Writes the ids of the kk largest keys, ascending, to out[0 .. kk).
+template <int ITEMS>
+__device__ __forceinline__ void select_top(const uint32_t (&key)[ITEMS], int it, int kk, int32_t *out,
+                                           SelectSmem &sm) {
+    select_masks<ITEMS>(key, it, kk, sm, [&](int first, uint32_t m, int p) {
         while (m != 0u) {
             out[p++] = first + __builtin_ctz(m);
             m &= m - 1u;
         }
-    }
+    });
 }
 
 }  // namespace sg
