@@ -174,23 +174,39 @@ __global__ __launch_bounds__(TOPK_THREADS) __attribute__((amdgpu_waves_per_eu(ev
         const int c = rank(k);                           // kept rows that stay
         m = k - c;
         int2 *mv = a.moves + unit * (cap / 2);
-        for (int i = 0; i < it; ++i) {
-            const int row = entry0 + i * 64;
-            if (row >= n) break;
-            const bool keep = (kept[row / 32] >> (row % 32)) & 1u;
-            const int r = rank(row);
-            if (row < k) {
-                if (!keep) {
-                    mv[row - r].x = row;
-                } else if (copy) {
-                    wo[row] = w[row];
-                    if (po) po[row] = ps[row];
+        for (int i0 = 0; i0 < it; i0 += STEP) {
+            // the rows' weights and positions, should they be written elsewhere;
+            // then what becomes of each (a row is read and written by its own
+            // thread, moves come later)
+            float x[STEP];
+            int32_t p[STEP];
+            if (copy) {
+#pragma unroll
+                for (int i = 0; i < STEP; ++i) {
+                    const int at = min(entry0 + (i0 + i) * 64, n - 1);
+                    x[i] = w[at];
+                    if (po) p[i] = ps[at];
                 }
-            } else if (keep) {
-                mv[r - c].y = row;                       // its weight goes with the move
-            } else {
-                wo[row] = 0.f;
-                if (po) po[row] = -1;
+            }
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) {
+                const int row = entry0 + (i0 + i) * 64;
+                if (i0 + i >= it || row >= n) break;
+                const bool keep = (kept[row / 32] >> (row % 32)) & 1u;
+                const int r = rank(row);
+                if (row < k) {
+                    if (!keep) {
+                        mv[row - r].x = row;
+                    } else if (copy) {
+                        wo[row] = x[i];
+                        if (po) po[row] = p[i];
+                    }
+                } else if (keep) {
+                    mv[r - c].y = row;                   // its weight goes with the move
+                } else {
+                    wo[row] = 0.f;
+                    if (po) po[row] = -1;
+                }
             }
         }
     } else {
