@@ -2,8 +2,8 @@
 // (fp4.h), with or without the weights the rows receive (decode_weights.h).
 //
 // Work.  Every (sequence, KV head) unit is cut into tiles of 32 rows, and the
-// tiles of all units stand in one line, of which up to D4_SHARES wavefronts
-// (eight per CU, all resident) take equal shares: the end of one unit, whole
+// tiles of all units stand in one line, of which as many wavefronts as the chip
+// holds (Plan4) take equal shares: the end of one unit, whole
 // units, the start of another.  A wavefront serves all G <= 16 query heads of a
 // unit and leaves a state for every unit it touches; a second launch joins
 // them.  Wavefronts are workgroups of their own: nothing waits for another, and
@@ -48,11 +48,21 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));     // outputs may start at any float
 
 constexpr int D4_TILE = 32;                  // rows per step
-constexpr int D4_NS = 4;                     // ring slots
 constexpr float D4_LAZY = 16.f;              // log2 headroom before the reference max is raised
-constexpr int D4_SHARES = 2048;              // wavefronts that share the tiles of all units
 constexpr int D4_MIN_SHARE = 2;              // tiles of a share at least
 constexpr int D4_SHARED_UNITS = 64 * 64;     // most units shared that way
+
+// Wavefronts of a launch and their rings.  Three wavefronts per SIMD with a ring
+// of two tiles stream as much as two with three, and hide more of the arithmetic's
+// latency (4.84 against 4.69 TB/s over 570 MB, 64 requests of 2,048 rows 39.6
+// against 40.7 us; deeper rings 0.8 to 0.9 of that); fp32 queries take registers
+// for two.
+template <typename T>
+struct Plan4 {
+    static constexpr int WAVES = sizeof(T) == 4 ? 2 : 3;      // per SIMD
+    static constexpr int NS = sizeof(T) == 4 ? 3 : 2;         // ring slots
+    static constexpr int SHARES = WAVES * 4 * 256;            // wavefronts that share the tiles of all units
+};
 
 // One ring slot: a tile's K codes, V codes and scales.
 template <int D>
@@ -60,7 +70,7 @@ struct Tile4 {
     static constexpr int CODES = D4_TILE * D / 2;
     static constexpr int SB = 2 * D / FP4_BLOCK;     // scale bytes per row: K's, then V's
     static constexpr int SLOT = 2 * CODES + 256;
-    static constexpr int LOADS = 2 * CODES / 1024 + 2;     // of a step, page entries included
+    static constexpr int LOADS = 2 * CODES / 1024 + 1;     // of a tile
 };
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const v4u &w) {
@@ -69,16 +79,18 @@ __device__ __forceinline__ bf16x8 as_bf16x8(const v4u &w) {
     return r;
 }
 
-// x cut into three parts of 8 significant bits each, as bf16 bits in the high
-// half: x = p[0] + p[1] + p[2] exactly (a part below the smallest normal is
-// lost).
+// x cut into three parts of 8 significant bits each, in the high halves of
+// p[0], p[1], p[2] (what the low halves hold does not count): their sum is x
+// (a part below the smallest normal is lost).
 __device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
-    p[0] = __float_as_uint(x) & 0xffff0000u;
-    const float r = x - __uint_as_float(p[0]);
-    p[1] = __float_as_uint(r) & 0xffff0000u;
-    p[2] = __float_as_uint(r - __uint_as_float(p[1])) & 0xffff0000u;
+    p[0] = __float_as_uint(x);
+    const float r = x - __uint_as_float(p[0] & 0xffff0000u);
+    p[1] = __float_as_uint(r);
+    p[2] = __float_as_uint(r - __uint_as_float(p[1] & 0xffff0000u));
 }
-__device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return (lo >> 16) | hi; }
+// The high halves of two words, or their low halves, as a pair.
+__device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100u); }
 
 // Direct global->LDS load of 4 bytes per lane: lane i's land at LDS offset
 // lds + 4 i (see dma16 in sg_internal.h).
@@ -87,6 +99,19 @@ __device__ __forceinline__ void dma4(const void *src, unsigned lds) {
 }
 __device__ __forceinline__ void dma4_nt(const void *src, unsigned lds) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off nt" ::"v"(src), "{m0}"(lds) : "memory");
+}
+
+// The same loads from a uniform base and a 32-bit offset per lane.  (Five wait
+// states: a scalar register that a vector instruction wrote may not be read by
+// a load before, and the compiler does not look into the assembly.)
+__device__ __forceinline__ void dma16_nt(const void *base, unsigned off, unsigned lds) {
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+
+// A uniform load through the scalar cache of data that nothing writes during
+// the kernel (the constant address space says so).
+__device__ __forceinline__ int32_t scalar_load(const int32_t *p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(reinterpret_cast<uintptr_t>(p));
 }
 
 struct Decode4Args {
@@ -112,72 +137,74 @@ struct Cursor4 {
 };
 
 // T: type of the queries; KEEP: the logits are kept for the weights and every
-// unit leaves a state; SHARED: wavefronts share the tiles of all units.
-template <typename T, int D, bool KEEP, bool SHARED>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void decode4_kernel(Decode4Args a) {
+// unit leaves a state; SHARED: wavefronts share the tiles of all units; HALVES:
+// pages are multiples of 16 rows, so each half of a tile lies in one page.
+template <typename T, int D, bool KEEP, bool SHARED, bool HALVES>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WAVES))) void decode4_kernel(Decode4Args a) {
     using L = Tile4<D>;
     constexpr int STEPS = D / 32;            // K products per 16 rows: 8 channels of every lane each
     constexpr int NC = D / 16;               // V channels per lane, and products per 32 rows
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    constexpr int NS = D4_NS, SB = L::SB;
-    static_assert((NS - 1) * L::LOADS <= 63, "loads in flight");
+    constexpr int NS = Plan4<T>::NS, SB = L::SB;
+    static_assert((NS - 1) * (L::LOADS + 1) <= 63, "loads in flight");
     __shared__ __attribute__((aligned(16))) char ring[NS * L::SLOT];
-    __shared__ int32_t entries[NS][64];      // page entries of a tile's rows (each twice)
+    __shared__ int32_t entries[HALVES ? 1 : NS][64];      // page entries of a tile's rows (each twice)
 
     const int lane = threadIdx.x, n16 = lane % 16, kg = lane / 16;
     const int Hq = a.Hq, Hkv = a.Hkv, G = Hq / Hkv, page_size = a.page_size;
     const int64_t max_rows = (int64_t)a.max_pages * page_size;
     auto rows_of = [&](int u) { return (int)max<int64_t>(0, min<int64_t>((int64_t)a.n_rows[u], max_rows)); };
+    auto rows_of_unit = [&](int u) { return (int)max<int64_t>(0, min<int64_t>((int64_t)scalar_load(a.n_rows + u), max_rows)); };
     auto tiles_of = [](int n) { return (n + D4_TILE - 1) / D4_TILE; };
-    auto scan64 = [&](int64_t x) {
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = __shfl_up(x, o, 64);
-            x += lane >= o ? y : 0;
-        }
-        return x;
-    };
-
     Cursor4 cur{(int)blockIdx.x, 0, 0, 0};
-    int near = 0, n_near = 0;                // lane i: rows of unit near + i
+    int near = 0, n_near = 0, window = 64;   // lane i < window: rows of unit near + i
     if constexpr (SHARED) {
         // The tile this share starts with: lane t sums the tiles of units
         // [t * per, (t + 1) * per); the lane whose range holds it, then the unit.
         const int per = (a.units + 63) / 64;         // at most 64
-        int64_t mine = 0;
-        for (int i0 = 0; i0 < per; i0 += 8) {
+        int mine = 0, first8[8];
+        auto rows8 = [&](int i0, int (&n)[8]) {
             int c[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int u = lane * per + i0 + i;
-                c[i] = a.n_rows[min(u, a.units - 1)];
-            }
+            for (int i = 0; i < 8; ++i) c[i] = a.n_rows[min(lane * per + i0 + i, a.units - 1)];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int u = lane * per + i0 + i;
-                const int n = (int)max<int64_t>(0, min<int64_t>(c[i], max_rows));
-                mine += i0 + i < per && u < a.units ? tiles_of(n) : 0;
+                const bool in = i0 + i < per && lane * per + i0 + i < a.units;
+                n[i] = in ? (int)max<int64_t>(0, min<int64_t>(c[i], max_rows)) : 0;
+                mine += tiles_of(n[i]);
             }
+        };
+        rows8(0, first8);
+        for (int i0 = 8; i0 < per; i0 += 8) {
+            int n[8];
+            rows8(i0, n);
         }
-        const int64_t upto = scan64(mine);
-        const int64_t total = __shfl(upto, 63, 64);
+        const int upto = wave_scan_incl(mine), total = __builtin_amdgcn_readlane(upto, 63);      // below 2^31
         // (never a share without a tile: a unit's states lie side by side)
-        const int64_t shares = max<int64_t>(1, min<int64_t>(gridDim.x, total / D4_MIN_SHARE));
-        if (blockIdx.x >= shares || total == 0) return;
-        const int64_t p0 = total * blockIdx.x / shares, p1 = total * (blockIdx.x + 1) / shares;
+        const int shares = max(1, min((int)gridDim.x, total / D4_MIN_SHARE)), share = (int)blockIdx.x;
+        if (share >= shares || total == 0) return;
+        // total / shares tiles each, the first total % shares one more
+        const int each = total / shares, more = total - each * shares;
+        const int p0 = share * each + min(share, more), p1 = p0 + each + (share < more ? 1 : 0);
         const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < upto)) - 1);
-        const int64_t before = __shfl(upto - mine, at, 64);
+        const int before = __builtin_amdgcn_readlane(upto - mine, at);
         near = at * per;
-        n_near = near + lane < a.units ? rows_of(near + lane) : 0;
+        if (per <= 8) {                      // the lane that sums them has them
+            window = per;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n_near = lane == i ? __builtin_amdgcn_readlane(first8[i], at) : n_near;
+        } else {
+            n_near = near + lane < a.units ? rows_of(near + lane) : 0;
+        }
         const int t = lane < per ? tiles_of(n_near) : 0;
-        const int64_t end = before + scan64(t);
+        const int end = before + wave_scan_incl(t);
         const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < end)) - 1);
         cur.unit = near + i;
         cur.n = __builtin_amdgcn_readlane(n_near, i);
-        cur.tile = __builtin_amdgcn_readfirstlane((int)(p0 - __shfl(end - t, i, 64)));
-        cur.left = __builtin_amdgcn_readfirstlane((int)(p1 - p0));
+        cur.tile = p0 - __builtin_amdgcn_readlane(end - t, i);
+        cur.left = p1 - p0;
     } else {
-        cur.n = rows_of(cur.unit);
+        cur.n = rows_of_unit(cur.unit);
         cur.left = tiles_of(cur.n);
     }
     auto advance = [&](Cursor4 &c) {
@@ -186,36 +213,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
         c.tile = 0;
         do {
             ++c.unit;                        // tiles are left, so units with rows are
-            c.n = c.unit - near < 64 ? __builtin_amdgcn_readlane(n_near, c.unit - near) : rows_of(c.unit);
+            c.n = c.unit - near < window ? __builtin_amdgcn_readlane(n_near, c.unit - near) : rows_of_unit(c.unit);
         } while (c.n == 0);
     };
 
-    // Row of a tile that a lane stands for, its page and its place there
-    auto locate = [&](const Cursor4 &c, int &lr, uint32_t &page, int &off) {
-        lr = c.tile * D4_TILE + lane % 32;
-        const uint32_t in = (uint32_t)min(lr, c.n - 1);
-        page = (uint32_t)(((uint64_t)in * a.page_mul) >> a.page_shift);
-        off = (int)(in - page * (uint32_t)page_size);
-    };
-    auto issue_entries = [&](const Cursor4 &c, int slot) {
-        int lr, off;
-        uint32_t page;
-        locate(c, lr, page, off);
-        dma4(a.page_table + (int64_t)c.unit * a.max_pages + page, lds_addr(&entries[slot][0]));
-    };
-    // Loads of a tile's rows into a ring slot.  Lane i stands for row i % 32: its
-    // pool row goes round by lane permutes.  A row that is left out (past the
-    // unit's rows or the share, or outside the pool) reads pool row 0, its bit in
-    // `valid` is clear.
-    unsigned valid = 0u;
-    auto issue_rows = [&](const Cursor4 &c, int slot) {
-        int lr, off;
-        uint32_t page;
-        locate(c, lr, page, off);
-        const int64_t x = (int64_t)entries[slot][lane] + off;
-        const bool ok = c.left > 0 && lr < c.n && x >= 0 && x < a.pool_rows;
-        const int row = ok ? (int)x : 0;
-        valid = (valid & ~(1u << slot)) | ((ok ? 1u : 0u) << slot);
+    unsigned valid = 0u;     // bit s: the row of slot s's tile that this lane stands for counts
+    unsigned full = 0u;      // bit s: every row of slot s's tile counts
+    // Loads of a tile whose row i lies at pool row `row` of lanes i and i + 32.
+    auto load_rows = [&](int row, int slot) {
         const unsigned base = lds_addr(ring + slot * L::SLOT);
         if constexpr (D == 128) {
             const int m4 = lane / 4, piece = lane % 4;
@@ -238,6 +243,75 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
             const int64_t vr = __shfl(row, (p / 16) * 16 + (p % 4) * 4 + (p % 16) / 4, 64);
             dma16_nt(a.v_pool + vr * 32 + piece * 16, base + L::CODES);
             dma4_nt(a.s_pool + (int64_t)row * 4, base + 2 * L::CODES);     // lanes 32 .. 63: the same again
+        }
+    };
+    // The same where the halves of the tile are 16 consecutive pool rows each,
+    // from x0 and x1 on: nothing but the scales' addresses takes vector work.
+    const unsigned k_off = D == 128 ? lane / 4 * 64 + (lane % 4 ^ lane / 16) * 16 : lane % 32 * 16;
+    const unsigned v_off = D == 128 ? (lane / 4 % 4 * 4 + lane / 16) * 64 + lane % 4 * 16
+                                    : (lane / 2 % 4 * 4 + lane / 2 % 16 / 4) * 32 + lane % 2 * 16;
+    auto load_halves = [&](int x0, int x1, int slot) {
+        const unsigned base = lds_addr(ring + slot * L::SLOT);
+        if constexpr (D == 128) {
+            dma16_nt(a.k_pool + (int64_t)x0 * 64, k_off, base);
+            dma16_nt(a.k_pool + (int64_t)x1 * 64, k_off, base + 1024);
+            dma16_nt(a.v_pool + (int64_t)x0 * 64, v_off, base + L::CODES);
+            dma16_nt(a.v_pool + (int64_t)x1 * 64, v_off, base + L::CODES + 1024);
+            const int64_t x = lane < 32 ? x0 : x1;
+            dma4_nt(a.s_pool + x * 8 + lane % 32 * 4, base + 2 * L::CODES);
+        } else {
+            // lanes 0 .. 31 the first half, 32 .. 63 the second
+            const int64_t x = lane < 32 ? x0 : x1;
+            dma16_nt(a.k_pool + x * 32 + k_off, base);
+            dma16_nt(a.v_pool + x * 32 + v_off, base + L::CODES);
+            const int64_t y = lane % 32 < 16 ? x0 : x1;
+            dma4_nt(a.s_pool + (y + lane % 16) * 4, base + 2 * L::CODES);
+        }
+    };
+    // Row of a tile that a lane stands for, its page and its place there
+    auto locate = [&](const Cursor4 &c, int &lr, uint32_t &page, int &off) {
+        lr = c.tile * D4_TILE + lane % 32;
+        const uint32_t in = (uint32_t)min(lr, c.n - 1);
+        page = (uint32_t)(((uint64_t)in * a.page_mul) >> a.page_shift);
+        off = (int)(in - page * (uint32_t)page_size);
+    };
+    auto issue_entries = [&](const Cursor4 &c, int slot) {
+        int lr, off;
+        uint32_t page;
+        locate(c, lr, page, off);
+        dma4(a.page_table + (int64_t)c.unit * a.max_pages + page, lds_addr(&entries[slot][0]));
+    };
+    // Loads of a tile's rows into a ring slot.  A row that is left out (past the
+    // unit's rows or the share, or outside the pool) reads pool row 0.
+    auto issue_rows = [&](const Cursor4 &c, int slot) {
+        int lr, off;
+        uint32_t page;
+        locate(c, lr, page, off);
+        const int64_t x = (int64_t)entries[slot][lane] + off;
+        const bool ok = c.left > 0 && lr < c.n && x >= 0 && x < a.pool_rows;
+        valid = (valid & ~(1u << slot)) | ((ok ? 1u : 0u) << slot);
+        full &= ~(1u << slot);
+        load_rows(ok ? (int)x : 0, slot);
+    };
+    // Pool rows of the halves of a tile (below 2^32, as the entries give them)
+    auto half_rows = [&](const Cursor4 &c, int64_t &x0, int64_t &x1) {
+        const int32_t *pt = a.page_table + (int64_t)c.unit * a.max_pages;
+        const uint32_t r0 = (uint32_t)c.tile * D4_TILE, r1 = r0 + 16 < (uint32_t)c.n ? r0 + 16 : r0;
+        const uint32_t p0 = (uint32_t)(((uint64_t)r0 * a.page_mul) >> a.page_shift);
+        const uint32_t p1 = (uint32_t)(((uint64_t)r1 * a.page_mul) >> a.page_shift);
+        x0 = (int64_t)scalar_load(pt + p0) + (int)(r0 - p0 * (uint32_t)page_size);
+        x1 = (int64_t)scalar_load(pt + p1) + (int)(r1 - p1 * (uint32_t)page_size);
+    };
+    auto issue_halves = [&](const Cursor4 &c, int64_t x0, int64_t x1, int slot) {
+        if (c.left > 0 && (c.tile + 1) * D4_TILE <= c.n && min(x0, x1) >= 0 && max(x0, x1) + 16 <= a.pool_rows) {
+            full |= 1u << slot;
+            load_halves((int)x0, (int)x1, slot);
+        } else {
+            const int64_t x = (lane % 32 < 16 ? x0 : x1) + lane % 16;
+            const bool ok = c.left > 0 && c.tile * D4_TILE + lane % 32 < c.n && x >= 0 && x < a.pool_rows;
+            valid = (valid & ~(1u << slot)) | ((ok ? 1u : 0u) << slot);
+            full &= ~(1u << slot);
+            load_rows(ok ? (int)x : 0, slot);
         }
     };
 
@@ -307,38 +381,62 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
         }
     };
 
-    begin_unit(cur.unit);
     if (cur.left == 0) {                     // a whole unit without rows
+        begin_unit(cur.unit);
         end_unit(cur.unit, true);
         return;
     }
     Cursor4 rows = cur, ents = cur;
     const int steps = cur.left;
+    int64_t x0 = 0, x1 = 0;                  // halves of the tile `rows` stands at
+    if constexpr (HALVES) {
+        half_rows(rows, x0, x1);
+        begin_unit(cur.unit);
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) {
-        issue_entries(ents, s);
-        advance(ents);
-    }
-    wait_vmem<0>();
+        for (int s = 0; s < NS - 1; ++s) {
+            issue_halves(rows, x0, x1, s);
+            advance(rows);
+            half_rows(rows, x0, x1);
+        }
+    } else {
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) {
-        issue_rows(rows, s);
-        advance(rows);
-        issue_entries(ents, (s + NS - 1) % NS);
-        advance(ents);
+        for (int s = 0; s < NS - 1; ++s) {
+            issue_entries(ents, s);
+            advance(ents);
+        }
+        begin_unit(cur.unit);                // its queries on the same round trip
+        wait_vmem<0>();
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s) {
+            issue_rows(rows, s);
+            advance(rows);
+            issue_entries(ents, (s + NS - 1) % NS);
+            advance(ents);
+        }
     }
     for (int st = 0; st < steps; ++st) {
-        // the rows of this step and the entries of the rows issued below; what
-        // else has been issued since (logits, states) only makes this stricter
-        wait_vmem<(NS - 2) * L::LOADS>();
-        issue_rows(rows, (st + NS - 1) % NS);
-        advance(rows);
-        issue_entries(ents, (st + NS - 2) % NS);
-        advance(ents);
+        // This step's rows (and the entries of the rows issued next) have
+        // landed: what else was issued since, logits and states, only makes the
+        // wait stricter.
+        if constexpr (HALVES) {
+            issue_halves(rows, x0, x1, (st + NS - 1) % NS);
+            advance(rows);
+            half_rows(rows, x0, x1);
+            // (two stores of logits in every step once the ring has gone round)
+            if (KEEP && st >= NS - 1) wait_vmem<(NS - 1) * (L::LOADS + 2)>();
+            else wait_vmem<(NS - 1) * L::LOADS>();
+        } else {
+            wait_vmem<(NS - 2) * (L::LOADS + 1)>();
+            issue_rows(rows, (st + NS - 1) % NS);
+            advance(rows);
+            issue_entries(ents, (st + NS - 2) % NS);
+            advance(ents);
+        }
         const int slot = st % NS;
                         const char *sb = ring + slot * L::SLOT;
                         const uint8_t *sc = reinterpret_cast<const uint8_t *>(sb + 2 * L::CODES);
-                        const uint32_t live = (uint32_t)__ballot((valid >> slot) & 1u);      // bit i: row i of the tile counts
+                        // bit i: row i of the tile counts
+        const uint32_t live = (full >> slot) & 1u ? 0xffffffffu : (uint32_t)__ballot((valid >> slot) & 1u);
                         // logits: lane (n16, kg) of half u gets rows 16 u + 4 kg + i of head n16
                         float z[8];
 #pragma unroll
@@ -368,7 +466,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
                                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][s], acc, 0, 0, 0);
                             }
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i] * a.scale_log2;
+                            for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i];         // unscaled
                         }
                         if (live != 0xffffffffu) {
 #pragma unroll
@@ -381,12 +479,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
 #pragma unroll
                                 for (int u = 0; u < 2; ++u)
                                     *reinterpret_cast<float4 *>(zp + 16 * u) =
-                                        make_float4(z[4 * u], z[4 * u + 1], z[4 * u + 2], z[4 * u + 3]);
+                                        make_float4(z[4 * u] * a.scale_log2, z[4 * u + 1] * a.scale_log2, z[4 * u + 2] * a.scale_log2,
+                                    z[4 * u + 3] * a.scale_log2);
                             }
                         }
                         float top = z[0];
 #pragma unroll
                         for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+        top *= a.scale_log2;
                         if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
                             top = fmaxf(top, __shfl_xor(top, 16, 64));
                             top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -405,7 +505,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
                         uint32_t pw[3][8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float p = __builtin_amdgcn_exp2f(z[i] - ref);
+                            const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale_log2, -ref));
                             l += p;
                             uint32_t x[3];
                             split3(p, x);
@@ -443,9 +543,9 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
                             v4u w;
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                w[i] = __builtin_amdgcn_perm(vb[2 * i + 1][j / 2], vb[2 * i][j / 2],
-                                                             j % 2 == 0 ? 0x05040100u : 0x07060302u);
-                            const bf16x8 vf = as_bf16x8(w);
+                                w[i] = j % 2 == 0 ? low_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2])
+                                  : high_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2]);
+            const bf16x8 vf = as_bf16x8(w);
 #pragma unroll
                             for (int k = 0; k < 3; ++k)
                                 o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[k], vf, o[j], 0, 0, 0);
@@ -465,22 +565,24 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void de
 }
 
 // Whether wavefronts share the tiles of all units: where a unit could be cut,
-// and the units are not too many for the lookup (64 per lane; the chip holds
-// 2,048 wavefronts).
+// the units are not too many for the lookup (64 per lane, more than the chip
+// holds wavefronts) and the tiles can be counted in 31 bits.
 static bool shares_tiles(int64_t units, int64_t max_rows) {
-    return max_rows > D4_MIN_SHARE * D4_TILE && units <= D4_SHARED_UNITS;
+    return max_rows > D4_MIN_SHARE * D4_TILE && units <= D4_SHARED_UNITS &&
+           units * ceil_div(max_rows, D4_TILE) <= 0x7fffffffll;
 }
 // Wavefronts that share them (the kernel uses fewer where the units are short).
+template <typename T>
 static int64_t shared_waves(int64_t units, int64_t max_rows) {
-    return std::max<int64_t>(1, std::min<int64_t>(D4_SHARES, units * ceil_div(max_rows, D4_TILE) / D4_MIN_SHARE));
+    return std::max<int64_t>(1, std::min<int64_t>(Plan4<T>::SHARES, units * ceil_div(max_rows, D4_TILE) / D4_MIN_SHARE));
 }
 
-struct Decode4Sizes {      // bytes of the workspace's parts
+struct Decode4Sizes {      // bytes of the workspace's parts (for either type of queries)
     size_t z, states, spans;
 };
 static Decode4Sizes decode4_sizes(int64_t units, int G, int d, int64_t max_rows, bool weights) {
     const bool shared = shares_tiles(units, max_rows);
-    const size_t slots = shared ? (size_t)(units + shared_waves(units, max_rows)) : weights ? (size_t)units : 0;
+    const size_t slots = shared ? (size_t)(units + shared_waves<uint16_t>(units, max_rows)) : weights ? (size_t)units : 0;
     return {weights ? (size_t)units * G * z_stride_of(max_rows) * sizeof(float) : 0,
             slots * G * (size_t)(d + 2) * sizeof(float), shared ? (size_t)units * sizeof(int2) : 0};
 }
@@ -499,8 +601,13 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     a.z_stride = w.z_stride = z_stride_of(max_rows);
     a.spans = shared ? reinterpret_cast<int2 *>(ws + sz.z) : nullptr;
     a.states = reinterpret_cast<float *>(ws + sz.z + sz.spans);
-    const unsigned grid = shared ? (unsigned)shared_waves(units, max_rows) : (unsigned)units;
-#define SG_D4(KEEP, SHARED) decode4_kernel<T, D, KEEP, SHARED><<<grid, 64, 0, s>>>(a)
+    const unsigned grid = shared ? (unsigned)shared_waves<T>(units, max_rows) : (unsigned)units;
+    const bool halves = a.page_size % 16 == 0;
+#define SG_D4(KEEP, SHARED)                                                           \
+    do {                                                                              \
+        if (halves) decode4_kernel<T, D, KEEP, SHARED, true><<<grid, 64, 0, s>>>(a);  \
+        else decode4_kernel<T, D, KEEP, SHARED, false><<<grid, 64, 0, s>>>(a);        \
+    } while (0)
     if (weights && shared) SG_D4(true, true);
     else if (weights) SG_D4(true, false);
     else if (shared) SG_D4(false, true);

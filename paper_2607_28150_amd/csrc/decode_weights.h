@@ -47,7 +47,7 @@ __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_
 // weights has its output already.
 //
 // Latency alone for small calls: the loads of a step are issued together (row
-// count and span, then eight states; for the weights the rows' logits of four
+// count and span, then sixteen states; for the weights the rows' logits of four
 // heads), so either kind of block takes three round trips.
 template <int D>
 constexpr int merge_blocks(int G) { return (G * D + FINISH_THREADS - 1) / FINISH_THREADS; }
@@ -62,7 +62,7 @@ template <int D>
 static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
     int G, int nsplit, const int32_t *__restrict__ n_rows, int64_t max_rows, int64_t split_rows,
     const int2 *__restrict__ spans, const float *__restrict__ states, float *__restrict__ out, Weights w) {
-    constexpr int GROUP = 8;       // states whose loads are in flight together
+    constexpr int GROUP = 16;      // states whose loads are in flight together
     const int64_t unit = blockIdx.x;
     const int2 sp = spans ? spans[unit] : make_int2(0, 0);
     const int64_t n = max<int64_t>(0, min<int64_t>(n_rows[unit], max_rows));

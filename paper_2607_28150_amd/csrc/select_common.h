@@ -45,17 +45,6 @@ __device__ __forceinline__ uint32_t order_key(float f) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// DPP lane moves of a wavefront scan: row shifts by 1, 2, 4, 8, then the last
-// lane of a row to the next rows.
-#define SG_SCAN_STEPS(STEP) STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
-
-// inclusive sum over the 64 lanes
-__device__ __forceinline__ int wave_scan_incl(int x) {
-#define SG_STEP(C, R) x += __builtin_amdgcn_update_dpp(0, x, C, R, 0xf, false);
-    SG_SCAN_STEPS(SG_STEP)
-#undef SG_STEP
-    return x;
-}
 // largest / smallest over the 64 lanes, in lane 63
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
 #define SG_STEP(C, R) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, C, R, 0xf, false));

@@ -101,6 +101,17 @@ __device__ __forceinline__ int wave_sum_int(int x) {
     return x;
 }
 
+// DPP lane moves of a wavefront scan: row shifts by 1, 2, 4, 8, then the last
+// lane of a row to the next rows.
+#define SG_SCAN_STEPS(STEP) STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
+
+// inclusive sum over the 64 lanes
+__device__ __forceinline__ int wave_scan_incl(int x) {
+#define SG_STEP(C, R) x += __builtin_amdgcn_update_dpp(0, x, C, R, 0xf, false);
+    SG_SCAN_STEPS(SG_STEP)
+#undef SG_STEP
+    return x;
+}
 __device__ __forceinline__ uint64_t lanemask_lt() {
     const unsigned lane = __lane_id();
     return lane == 0 ? 0ull : (~0ull >> (64 - lane));
