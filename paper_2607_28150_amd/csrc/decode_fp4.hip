@@ -180,8 +180,13 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
             rows8(i0, n);
         }
         const int upto = wave_scan_incl(mine), total = __builtin_amdgcn_readlane(upto, 63);      // below 2^31
-        // (never a share without a tile: a unit's states lie side by side)
-        const int shares = max(1, min((int)gridDim.x, total / D4_MIN_SHARE)), share = (int)blockIdx.x;
+        // Tiles of a share, at least: its time goes with them, that of joining a
+        // unit's shares with their number, so a part of the root of a unit's tiles
+        // (of 0, 0.3, 0.5 and 1 times the root, one request of 32,768 rows 36, 28.5,
+        // 31.3 and 46.5 us, of 819 rows within 1 us for the first three).  Never a
+        // share without a tile: a unit's states lie side by side.
+        const int tiles = max(D4_MIN_SHARE, (int)(0.3f * sqrtf((float)total / (float)a.units)));
+        const int shares = max(1, min((int)gridDim.x, total / tiles)), share = (int)blockIdx.x;
         if (share >= shares || total == 0) return;
         // total / shares tiles each, the first total % shares one more
         const int each = total / shares, more = total - each * shares;
@@ -422,9 +427,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
             issue_halves(rows, x0, x1, (st + NS - 1) % NS);
             advance(rows);
             half_rows(rows, x0, x1);
-            // (two stores of logits in every step once the ring has gone round)
-            if (KEEP && st >= NS - 1) wait_vmem<(NS - 1) * (L::LOADS + 2)>();
-            else wait_vmem<(NS - 1) * L::LOADS>();
+            wait_vmem<(NS - 1) * L::LOADS>();
         } else {
             wait_vmem<(NS - 2) * (L::LOADS + 1)>();
             issue_rows(rows, (st + NS - 1) % NS);
@@ -613,10 +616,8 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     else if (shared) SG_D4(false, true);
     else SG_D4(false, false);
 #undef SG_D4
-    if (weights || shared) {
-        decode_finish_kernel<D><<<finish_grid<D>(units, G, weights, max_rows), FINISH_THREADS, 0, s>>>(
-            G, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
-    }
+    if (weights || shared)
+        launch_finish<D>(s, units, G, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
     return launch_status(fn);
 }
 

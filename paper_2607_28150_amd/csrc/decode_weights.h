@@ -18,8 +18,6 @@
 
 namespace sg {
 
-constexpr int FINISH_THREADS = 256;
-constexpr int FINISH_ROWS = FINISH_THREADS * 4;      // rows per workgroup
 constexpr int FINISH_MAX_G = 16;
 
 struct Weights {
@@ -40,34 +38,26 @@ __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_
     return split_rows > 0 ? (int)min<int64_t>(nsplit, ceil_div(n, split_rows)) : (n > 0 ? nsplit : 0);
 }
 
-// Grid: x = unit; y below merge_blocks(G): FINISH_THREADS / D heads' outputs,
-// then chunks of FINISH_ROWS rows' weights.  States of a unit: nsplit places, of
+// Grid: x = unit; y below G: a head's outputs, THREADS / D threads per channel
+// sharing its states; then chunks of 4 * THREADS rows' weights.  States of a unit: nsplit places, of
 // which the used ones come first; or, with `spans`, places unit +
 // spans[unit].x .. unit + spans[unit].y, where a unit with one state and no
 // weights has its output already.
 //
 // Latency alone for small calls: the loads of a step are issued together (row
-// count and span, then sixteen states; for the weights the rows' logits of four
-// heads), so either kind of block takes three round trips.
-template <int D>
-constexpr int merge_blocks(int G) { return (G * D + FINISH_THREADS - 1) / FINISH_THREADS; }
-
-template <int D>
-static dim3 finish_grid(int64_t units, int G, bool weights, int64_t max_rows) {
-    return dim3((unsigned)units,
-                (unsigned)(merge_blocks<D>(G) + (weights ? ceil_div(max_rows, FINISH_ROWS) : 0)));
-}
-
-template <int D>
-static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
+// count and span, then eight states per thread; for the weights the rows' logits
+// of four heads), so either kind of block takes three round trips.
+template <int D, int THREADS>
+static __global__ __launch_bounds__(THREADS) void decode_finish_kernel(
     int G, int nsplit, const int32_t *__restrict__ n_rows, int64_t max_rows, int64_t split_rows,
     const int2 *__restrict__ spans, const float *__restrict__ states, float *__restrict__ out, Weights w) {
-    constexpr int GROUP = 16;      // states whose loads are in flight together
+    constexpr int GROUP = 8;       // states whose loads are in flight together
+    constexpr int ROWS = THREADS * 4;
     const int64_t unit = blockIdx.x;
     const int2 sp = spans ? spans[unit] : make_int2(0, 0);
     const int64_t n = max<int64_t>(0, min<int64_t>(n_rows[unit], max_rows));
-    const int chunk = (int)blockIdx.y - merge_blocks<D>(G);
-    if (chunk >= 0 && (int64_t)chunk * FINISH_ROWS >= n) return;       // uniform
+    const int chunk = (int)blockIdx.y - G;
+    if (chunk >= 0 && (int64_t)chunk * ROWS >= n) return;       // uniform
     int used = used_splits(n, nsplit, split_rows);
     int64_t first = unit * nsplit;
     if (spans && n > 0) {
@@ -79,11 +69,19 @@ static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
     const int64_t step = (int64_t)G * (D + 2);
 
     if (chunk < 0) {
-        const int g = (int)blockIdx.y * (FINISH_THREADS / D) + threadIdx.x / D, c = threadIdx.x % D;
-        if (g >= G) return;
+        constexpr int SHARE = THREADS / D;
+        __shared__ float part[SHARE][3][D];      // max, sum and output of each thread's states
+        const int g = blockIdx.y, c = threadIdx.x % D, k = threadIdx.x / D;
         const float *p = st + (int64_t)g * (D + 2);
         float M = -INFINITY, L = 0.f, O = 0.f;
-        for (int s0 = 0; s0 < used; s0 += GROUP) {
+        auto join = [&](float m, float l, float o) {       // in a fixed order
+            const float top = fmaxf(M, m);
+            const float f = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top), a = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            L = f * L + a * l;
+            O = f * O + a * o;
+            M = top;
+        };
+        for (int s0 = k * GROUP; s0 < used; s0 += SHARE * GROUP) {
             float m[GROUP], l[GROUP], o[GROUP];
 #pragma unroll
             for (int j = 0; j < GROUP; ++j) {
@@ -92,28 +90,25 @@ static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
                 l[j] = x[1];
                 o[j] = x[2 + c];
             }
-            float top = M;
-#pragma unroll
-            for (int j = 0; j < GROUP; ++j) top = fmaxf(top, m[j]);        // (past the last: it again)
-            const float f = M == top ? 1.f : __builtin_amdgcn_exp2f(M - top);
-            L *= f;
-            O *= f;
-            M = top;
 #pragma unroll
             for (int j = 0; j < GROUP; ++j)
-                if (s0 + j < used) {
-                    const float a = m[j] == M ? 1.f : __builtin_amdgcn_exp2f(m[j] - M);
-                    L += a * l[j];
-                    O += a * o[j];
-                }
+                if (s0 + j < used) join(m[j], l[j], o[j]);
         }
-        out[(unit * G + g) * D + c] = L == 0.f ? 0.f : O / L;
+        if (used > GROUP) {                      // uniform; else the first thread has them all
+            part[k][0][c] = M;
+            part[k][1][c] = L;
+            part[k][2][c] = O;
+            __syncthreads();
+            if (k == 0)
+                for (int j = 1; j < SHARE; ++j) join(part[j][0][c], part[j][1][c], part[j][2][c]);
+        }
+        if (k == 0) out[(unit * G + g) * D + c] = L == 0.f ? 0.f : O / L;
         return;
     }
 
     __shared__ float M_s[FINISH_MAX_G], inv_s[FINISH_MAX_G];
     const int lane = threadIdx.x % 64;
-    for (int g = threadIdx.x / 64; g < G; g += FINISH_THREADS / 64) {
+    for (int g = threadIdx.x / 64; g < G; g += THREADS / 64) {
         const float *p = st + (int64_t)g * (D + 2);
         float M = -INFINITY, L = 0.f;
         for (int s0 = 0; s0 < used; s0 += 64) {
@@ -134,7 +129,7 @@ static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
     __syncthreads();
     // four rows per thread, four heads at a time (rows past n lie within the
     // unit's logits, or are not read)
-    const int64_t i = (int64_t)chunk * FINISH_ROWS + threadIdx.x * 4;
+    const int64_t i = (int64_t)chunk * ROWS + threadIdx.x * 4;
     if (i >= n) return;
     float add[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
     const int64_t at = unit * w.stride + i;
@@ -158,6 +153,19 @@ static __global__ __launch_bounds__(FINISH_THREADS) void decode_finish_kernel(
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (i + j < n) w.out[at + j] = w.decay * old[j] + add[j];
+}
+
+// Four times the threads where few heads with many states each are joined; most
+// of them would idle where the heads fill the chip.
+template <int D>
+static void launch_finish(hipStream_t s, int64_t units, int G, int nsplit, const int32_t *n_rows, int64_t max_rows,
+                          int64_t split_rows, const int2 *spans, const float *states, float *out, const Weights &w) {
+    const int threads = units * G <= 2 * device_cus() ? 1024 : 256;
+    const dim3 grid((unsigned)units, (unsigned)(G + (w.out ? ceil_div(max_rows, threads * 4) : 0)));
+    if (threads == 1024)
+        decode_finish_kernel<D, 1024><<<grid, 1024, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
+    else
+        decode_finish_kernel<D, 256><<<grid, 256, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
 }
 
 }  // namespace sg

@@ -9,8 +9,14 @@
 
 namespace sg {
 
-constexpr int FETCH4_THREADS = 256;
-constexpr int FETCH4_UNROLL = 4;
+// One wavefront per workgroup, two entries per lane group: of 256 and 64
+// threads with one, two and four entries, the fastest for many rows (209,664
+// bf16 rows of d = 128 written in 28.8 us and read back in 31.0; 256 threads
+// with four entries 31.5 and 33.0) and next to it for few (512 rows 4.0 and
+// 4.2 us; 5.6 and 6.0).  From a host source: larger workgroups with more in
+// flight, see the launch.
+constexpr int FETCH4_THREADS = 64, FETCH4_UNROLL = 2;
+constexpr int FETCH4_HOST_THREADS = 256, FETCH4_HOST_UNROLL = 4;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_u32(uint32_t x) {
@@ -92,8 +98,8 @@ __device__ __forceinline__ uint2 gather_scales(uint32_t kb, uint32_t vb, int c) 
 }
 
 // SRC, DST: float, uint16_t (bf16) or F4; one of them is F4.
-template <typename SRC, typename DST, int D>
-__global__ __launch_bounds__(FETCH4_THREADS) void fetch4_kernel(
+template <typename SRC, typename DST, int D, int THREADS, int UNROLL>
+__global__ __launch_bounds__(THREADS) void fetch4_kernel(
     int rows, const int32_t *__restrict__ row_off, int64_t total, const int32_t *__restrict__ index,
     const int32_t *__restrict__ n_valid, const int64_t *__restrict__ src_row_base, int64_t src_rows,
     const void *__restrict__ k_src, const void *__restrict__ v_src, const uint8_t *__restrict__ s_src,
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(FETCH4_THREADS) void fetch4_kernel(
     void *__restrict__ k_pool, void *__restrict__ v_pool, uint8_t *__restrict__ s_pool, int64_t pool_rows) {
     constexpr bool FROM4 = std::is_same_v<SRC, F4>, TO4 = std::is_same_v<DST, F4>;
     constexpr int LPR = D / 8, SB = 2 * D / FP4_BLOCK;     // lanes and scale bytes of a row
-    constexpr int EPI = FETCH4_THREADS / LPR, EPB = EPI * FETCH4_UNROLL;
+    constexpr int EPI = THREADS / LPR, EPB = EPI * UNROLL;
     const int c = threadIdx.x % LPR, sub = threadIdx.x / LPR;
     if (src_rows <= 0) return;
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
@@ -114,17 +120,17 @@ __global__ __launch_bounds__(FETCH4_THREADS) void fetch4_kernel(
         for (int64_t base = (int64_t)blockIdx.y * EPB; base < n; base += (int64_t)gridDim.y * EPB) {
             // the index loads of the pass, then the row loads (an entry that is
             // not copied reads source row 0), then the stores
-            int64_t tok[FETCH4_UNROLL];
+            int64_t tok[UNROLL];
 #pragma unroll
-            for (int j = 0; j < FETCH4_UNROLL; ++j) {
+            for (int j = 0; j < UNROLL; ++j) {
                 const int64_t i = min(base + sub + j * EPI, n - 1);
                 tok[j] = index ? (int64_t)index[o + i] : i;
             }
-            Slice8<SRC> ks[FETCH4_UNROLL], vs[FETCH4_UNROLL];
-            uint2 sc[FETCH4_UNROLL];
-            int64_t dst[FETCH4_UNROLL];
+            Slice8<SRC> ks[UNROLL], vs[UNROLL];
+            uint2 sc[UNROLL];
+            int64_t dst[UNROLL];
 #pragma unroll
-            for (int j = 0; j < FETCH4_UNROLL; ++j) {
+            for (int j = 0; j < UNROLL; ++j) {
                 const int64_t i = base + sub + j * EPI, src = sbase + tok[j], lr = lbase + i;
                 const bool live = i < n && src >= 0 && src < src_rows;
                 const int64_t s_row = live ? src : 0;
@@ -141,7 +147,7 @@ __global__ __launch_bounds__(FETCH4_THREADS) void fetch4_kernel(
                 }
             }
 #pragma unroll
-            for (int j = 0; j < FETCH4_UNROLL; ++j) {
+            for (int j = 0; j < UNROLL; ++j) {
                 if constexpr (TO4) {
                     uint32_t kc, vc;
                     uint2 s;
@@ -221,21 +227,32 @@ extern "C" int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int 
     SG_REQUIRE(aligned16(k_src) && aligned16(v_src) && aligned16(s_src) && aligned16(k_pool) && aligned16(v_pool) &&
                    aligned16(s_pool),
                SG_EINVAL, "%s: row arrays must be 16-byte aligned", fn);
-    // workgroups per index row: one pass over a row of average length, more
-    // where the rows alone would leave the chip idle; longer rows are covered
-    // by the stride loop
-    const int64_t epb = FETCH4_THREADS / (d / 8) * FETCH4_UNROLL;
-    int64_t ny = std::max(ceil_div(ceil_div(total, rows), epb), std::min(ceil_div(total, epb), ceil_div(512, rows)));
-    dim3 grid((unsigned)std::min<int64_t>(rows, max_workgroups(FETCH4_THREADS)), (unsigned)std::min<int64_t>(ny, 65535));
-    if (host_memory(k_src) || host_memory(v_src)) {
-        grid.x = (unsigned)std::min(rows, HOST_LINK_WORKGROUPS);
-        grid.y = (unsigned)std::max(1, HOST_LINK_WORKGROUPS / (int)grid.x);
+    const bool host = host_memory(k_src) || host_memory(v_src);
+    dim3 grid;
+    if (!host) {
+        // workgroups per index row: one pass over a row of average length, more
+        // where the rows alone would leave the chip idle; longer rows are
+        // covered by the stride loop
+        const int64_t epb = FETCH4_THREADS / (d / 8) * FETCH4_UNROLL;
+        const int64_t ny = std::max(ceil_div(ceil_div(total, rows), epb), std::min(ceil_div(total, epb), ceil_div(2048, rows)));
+        grid = dim3((unsigned)std::min<int64_t>(rows, max_workgroups(FETCH4_THREADS)), (unsigned)std::min<int64_t>(ny, 65535));
+    } else {
+        // as many bytes in flight as sg_fetch has from a host source: HOST_LINK_WORKGROUPS
+        // times 256 threads with eight entries of two 16-byte vectors
+        const int slice = src_dt == SG_F32 ? 32 : src_dt == SG_BF16 ? 16 : 4;
+        const int wgs = HOST_LINK_WORKGROUPS * 8 * 16 / (FETCH4_HOST_UNROLL * slice);
+        grid = dim3((unsigned)std::min(rows, wgs), (unsigned)std::max(1, wgs / std::min(rows, wgs)));
     }
     hipStream_t s = as_stream(stream);
-#define SG_FETCH4(S, T, D)                                                                                           \
-    fetch4_kernel<S, T, D><<<grid, FETCH4_THREADS, 0, s>>>(rows, row_off, total, index, n_valid, src_row_base,       \
-                                                           src_rows, k_src, v_src, s_src, page_table, page_size,     \
-                                                           max_pages, dst_start, k_pool, v_pool, s_pool, pool_rows)
+#define SG_FETCH4_L(S, T, D, THREADS, UNROLL)                                                                          \
+    fetch4_kernel<S, T, D, THREADS, UNROLL><<<grid, THREADS, 0, s>>>(                                                  \
+        rows, row_off, total, index, n_valid, src_row_base, src_rows, k_src, v_src, s_src, page_table, page_size,      \
+        max_pages, dst_start, k_pool, v_pool, s_pool, pool_rows)
+#define SG_FETCH4(S, T, D)                                                                                             \
+    do {                                                                                                               \
+        if (host) SG_FETCH4_L(S, T, D, FETCH4_HOST_THREADS, FETCH4_HOST_UNROLL);                                       \
+        else SG_FETCH4_L(S, T, D, FETCH4_THREADS, FETCH4_UNROLL);                                                      \
+    } while (0)
 #define SG_FETCH4_D(S, T)                  \
     do {                                   \
         if (d == 64) SG_FETCH4(S, T, 64);  \
@@ -248,5 +265,6 @@ extern "C" int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int 
     else SG_FETCH4_D(F4, uint16_t);
 #undef SG_FETCH4_D
 #undef SG_FETCH4
+#undef SG_FETCH4_L
     return launch_status(fn);
 }

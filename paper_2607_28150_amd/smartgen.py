@@ -574,16 +574,18 @@ def _addresses(*tensors):
     for t in tensors:
         if t is None:
             out.append(None)
-        elif t.is_cuda:
-            if not t.is_contiguous():
-                raise ValueError("tensors passed to the library must be contiguous")
-            if t.get_device() != device:
-                device = torch.cuda.current_device()
-                if t.get_device() != device:
-                    raise ValueError(f"a tensor lies on {t.device}, the current device is {device}")
-            out.append(t.data_ptr())
-        else:
+            continue
+        at = t.get_device()
+        if at < 0:
             out.append(_ptr(t))
+            continue
+        if at != device:
+            device = torch.cuda.current_device()
+            if at != device:
+                raise ValueError(f"a tensor lies on {t.device}, the current device is {device}")
+        if not t.is_contiguous():
+            raise ValueError("tensors passed to the library must be contiguous")
+        out.append(t.data_ptr())
     return out
 
 
