@@ -804,7 +804,7 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
         w.z_stride = z_stride_of(max_rows);
         float *states = ws + zfloats;
         launch(decode_kernel<T, D, HG, true>, states, w.z, w.z_stride);
-        launch_finish<D>(s, units, G, (int)nsplit, n_rows, max_rows, split_rows, nullptr, states, out, w);
+        launch_finish<D>(s, units, G, nsplit, (int)nsplit, n_rows, max_rows, split_rows, nullptr, states, out, w);
         return launch_status(fn);
     }
     launch(decode_kernel<T, D, HG, false>, ws, nullptr, 0);

@@ -617,7 +617,7 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     else SG_D4(false, false);
 #undef SG_D4
     if (weights || shared)
-        launch_finish<D>(s, units, G, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
+        launch_finish<D>(s, units, G, shared ? grid / units + 1 : 1, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
     return launch_status(fn);
 }
 

@@ -155,17 +155,22 @@ static __global__ __launch_bounds__(THREADS) void decode_finish_kernel(
         if (i + j < n) w.out[at + j] = w.decay * old[j] + add[j];
 }
 
-// Four times the threads where few heads with many states each are joined; most
-// of them would idle where the heads fill the chip.
+// `expect`: states per unit.  As many threads as take them in one go, eight
+// each: a block of 1,024 threads for a head's few hundred, of 128 where every
+// unit has a handful and the heads fill the chip.
 template <int D>
-static void launch_finish(hipStream_t s, int64_t units, int G, int nsplit, const int32_t *n_rows, int64_t max_rows,
-                          int64_t split_rows, const int2 *spans, const float *states, float *out, const Weights &w) {
-    const int threads = units * G <= 2 * device_cus() ? 1024 : 256;
-    const dim3 grid((unsigned)units, (unsigned)(G + (w.out ? ceil_div(max_rows, threads * 4) : 0)));
-    if (threads == 1024)
-        decode_finish_kernel<D, 1024><<<grid, 1024, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
-    else
-        decode_finish_kernel<D, 256><<<grid, 256, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
+static void launch_finish(hipStream_t s, int64_t units, int G, int64_t expect, int nsplit, const int32_t *n_rows,
+                          int64_t max_rows, int64_t split_rows, const int2 *spans, const float *states, float *out,
+                          const Weights &w) {
+    auto launch = [&](auto kernel, int threads) {
+        const dim3 grid((unsigned)units, (unsigned)(G + (w.out ? ceil_div(max_rows, threads * 4) : 0)));
+        kernel<<<grid, threads, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
+    };
+    const int64_t threads = ceil_div(expect, 8) * D;
+    if (threads <= 128) launch(decode_finish_kernel<D, 128>, 128);
+    else if (threads <= 256) launch(decode_finish_kernel<D, 256>, 256);
+    else if (threads <= 512) launch(decode_finish_kernel<D, 512>, 512);
+    else launch(decode_finish_kernel<D, 1024>, 1024);
 }
 
 }  // namespace sg
