@@ -529,7 +529,9 @@ int sg_spec_commit(void *stream, int L, int Hkv, int64_t T, int64_t s0, int64_t 
  *
  *   s_src, s_pool  the scales, device (s_src: or pinned host) memory; required
  *           with SG_FP4 on that side and NULL otherwise.
- * All row arrays must be 16-byte aligned; source and pool must not overlap.
+ * All row arrays must be 16-byte aligned; source and pool must not overlap.  No
+ * two entries of a call may write one pool row (its codes and scales could come
+ * from different ones).
  */
 int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows, const int32_t *row_off,
                  int64_t total, const int32_t *index, const int32_t *n_valid, const int64_t *src_row_base,
@@ -558,8 +560,9 @@ int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows
  *   NULL (then weight_in too): attention alone.
  * A NaN row makes the outputs and weights of its unit NaN.
  *   ws      device workspace of at least the matching size, 16-byte aligned
- *           (logits of every row and split states); no initialisation needed,
- *           calls that share one must be ordered.  `weights` of the size call:
+ *           (with weights, 4 bytes per q head and row for the logits; split
+ *           states); no initialisation needed, calls that share one must be
+ *           ordered.  `weights` of the size call:
  *           whether weight_out is given.
  */
 size_t sg_decode_attn_acc_workspace_size(int B, int Hq, int Hkv, int d, int max_pages, int page_size);

@@ -610,11 +610,13 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         for (int w = 0; w < WAVES; ++w) M = fmaxf(M, m_s[w][g]);
         float Lsum = 0.f;
         float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (M > -INFINITY) {
+        if (ACC || M > -INFINITY) {
 #pragma unroll
             for (int wp = 0; wp < PW; ++wp) {
                 const int w = sub * PW + wp;
-                const float a = m_s[w][g] > -INFINITY ? __builtin_amdgcn_exp2f(m_s[w][g] - M) : 0.f;
+                // (a state of NaN rows alone has M = -inf and is not lost among the weights)
+                const float a = ACC ? (m_s[w][g] == M ? 1.f : __builtin_amdgcn_exp2f(m_s[w][g] - M))
+                                    : m_s[w][g] > -INFINITY ? __builtin_amdgcn_exp2f(m_s[w][g] - M) : 0.f;
                 const float lw = (l_s[4 * w][g] + l_s[4 * w + 1][g]) + (l_s[4 * w + 2][g] + l_s[4 * w + 3][g]);
                 const float4 x = *reinterpret_cast<const float4 *>(ring + w * (NS * SLOTB) + (g * D + cc) * 4);
                 Lsum = fmaf(a, lw, Lsum);

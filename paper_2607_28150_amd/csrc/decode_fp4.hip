@@ -646,7 +646,7 @@ extern "C" int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int 
     SG_REQUIRE(page_size >= 1 && max_pages >= 1 && pool_rows >= 0, SG_EINVAL, "%s: bad page geometry", fn);
     SG_REQUIRE((int64_t)max_pages * page_size <= (1ll << 30), SG_EINVAL, "%s: page table too large", fn);
     SG_REQUIRE(pool_rows <= 0x7fffffffll, SG_EUNSUPPORTED, "%s: pool above 2^31 rows", fn);
-    SG_REQUIRE(scale > 0.f && scale <= 3.4e38f, SG_EINVAL, "%s: scale must be positive and finite", fn);
+    SG_REQUIRE(scale > 0.f && scale <= 2e38f, SG_EINVAL, "%s: scale must be positive and finite", fn);
     SG_REQUIRE((int64_t)B * Hkv <= max_workgroups(64), SG_EUNSUPPORTED, "%s: too many units", fn);
     if (weight_out) {
         SG_REQUIRE(weight_stride >= (int64_t)max_pages * page_size, SG_EINVAL, "%s: weight rows of %lld floats hold no %lld rows",

@@ -422,3 +422,78 @@ def test_streams_and_graph():
         step()
         torch.cuda.synchronize()
         assert torch.equal(replayed, out) and torch.equal(wr, w) and torch.equal(out, first)
+
+
+@pytest.mark.parametrize("units,page", [(5000, 16), (4200, 10), (1500, 16), (700, 9)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_many_units(units, page, weights):
+    """More units than one lookup covers (a whole unit per wavefront), and the
+    lookup with several units per lane; empty units among them."""
+    say("many units", units, page, weights)
+    r = np.random.default_rng(units)
+    lens = np.where(r.random(units // 2) < 0.3, 0, r.integers(0, 100, units // 2))
+    lens[5:5 + min(300, units // 6)] = 0                # a long run of empty ones
+    c = Case(lens.tolist(), 4, 2, 64, page, "bf16", "fp4", seed=units, extra_pages=0)
+    c.check(None, 1.0, weights)
+
+
+@pytest.mark.parametrize("page", [16, 24])
+def test_attention_short_units_in_a_row(page):
+    """Shares that cross from unit to unit at every tile."""
+    say("short units", page)
+    c = Case([1 + i % 40 for i in range(256)], 3, 2, 128, page, "f32", "fp4", seed=page, extra_pages=3)
+    c.check(None, 1.0, True)
+
+
+def test_outputs_at_any_float():
+    say("outputs at any float")
+    for pool in ("fp4", "bf16"):
+        c = Case([300, 40], 4, 2, 128, 16, "bf16", pool, seed=5)
+        B, Hq, d = c.q.shape
+        rows, shape = c.table.shape[2] * 16, (2, Hq, 2, d, c.table.shape[2], 16)
+        flat, wflat = torch.zeros(B * Hq * d + 3, device="cuda"), torch.zeros(B * 2 * rows + 3, device="cuda")
+        out, w = flat[1:1 + B * Hq * d].view(B, Hq, d), wflat[3:].view(B, 2, rows)
+        if pool == "fp4":
+            ws = torch.empty(sg.decode_fp4_workspace_size(*shape, weights=True), dtype=torch.uint8, device="cuda")
+            sg.sg_decode_attn_fp4(c.q, *c.pools, cu(c.table), cu(c.n), 16, out, ws=ws, weight_out=w)
+        else:
+            ws = torch.empty(sg.decode_acc_workspace_size(*shape), dtype=torch.uint8, device="cuda")
+            sg.sg_decode_attn_acc(c.q, *c.pools, cu(c.table), cu(c.n), 16, out, w, ws)
+        want, wwant = c.run(None)
+        assert np.array_equal(out.cpu().numpy(), want)
+        for b, n in enumerate((300, 40)):
+            assert np.array_equal(w[b, :, :n].cpu().numpy(), wwant[b, :, :n])
+
+
+@pytest.mark.parametrize("pool", ["bf16", "f32", "fp4"])
+def test_only_nan_rows(pool):
+    say("only nan rows", pool)
+    c = Case([40, 40], 4, 1, 128, 16, "f32" if pool == "f32" else "bf16", pool, seed=3)
+    at = torch.from_numpy(ref.pool_rows_of(c.table[1, 0], 40, 16, c.pool_rows)).cuda()
+    if c.fp4:
+        c.pools[2][at] = 255
+    else:
+        c.pools[0][at] = float("nan")
+    out, w = c.run(None)
+    assert np.isnan(out[1]).all() and np.isnan(w[1, 0, :40]).all()
+    assert not np.isnan(out[0]).any() and not np.isnan(w[0]).any()
+
+
+def test_refused_where_it_would_not_fit():
+    """The calls' own checks with tensors on the GPU."""
+    say("refusals")
+    c = Case([300], 4, 2, 128, 16, "bf16", "fp4", seed=1)
+    table, n, out = cu(c.table), cu(c.n), torch.empty((1, 8, 128), device="cuda")
+    with pytest.raises(sg.SmartgenError, match="workspace"):
+        sg.sg_decode_attn_fp4(c.q, *c.pools, table, n, 16, out)
+    with pytest.raises(ValueError, match="contiguous"):
+        sg.sg_decode_attn_fp4(c.q.transpose(0, 1).contiguous().transpose(0, 1)[:, ::2], *c.pools, table, n, 16, out)
+    with pytest.raises(ValueError, match="n_rows"):
+        sg.sg_decode_attn_fp4(c.q, *c.pools, table, n.long(), 16, out)
+    with pytest.raises(ValueError, match="pinned"):
+        sg.sg_decode_attn_fp4(c.q, c.pools[0].cpu(), *c.pools[1:], table, n, 16, out)
+    with pytest.raises(sg.SmartgenError, match="group size"):
+        sg.sg_decode_attn_acc(c.q[:, :6].contiguous(), torch.zeros((64, 128), dtype=torch.bfloat16, device="cuda"),
+                              torch.zeros((64, 128), dtype=torch.bfloat16, device="cuda"), table, n, 16, out,
+                              torch.zeros((1, 2, c.table.shape[2] * 16), device="cuda"),
+                              torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))

@@ -137,6 +137,37 @@ def test_evict_many_units():
     check("bf16", 64, 16, lens, [min(64, max(0, n - 1)) for n in lens], weights(r, 700, 160, "spread"))
 
 
+@pytest.mark.parametrize("dtype,d", [("fp4", 128), ("fp4", 64), ("f32", 128), ("f32", 64), ("bf16", 128)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_units_move_their_own_rows(dtype, d, in_place):
+    """Units enough for every CU: one launch selects and moves."""
+    say("evict own rows", dtype, d, in_place)
+    r = np.random.default_rng(5)
+    lens = r.integers(0, 300, 280).tolist()
+    pos = np.stack([r.permutation(320) for _ in lens])
+    check(dtype, d, 16, lens, [n // 3 for n in lens], weights(r, 280, 320, "spread"), pos=pos, sinks=3,
+          recent=[300] * 280, in_place=in_place, seed=9)
+
+
+def test_evict_far_pool_rows():
+    """Pool rows whose byte offsets pass 32 bits."""
+    say("evict far rows")
+    rows, n, k = 72_000_000, 64, 32
+    t = [torch.zeros((rows, w), dtype=torch.uint8, device="cuda") for w in (64, 64, 8)]
+    for i, x in enumerate(t):
+        x[-n:] = (torch.arange(n, device="cuda") + 10 * i + 1).to(torch.uint8)[:, None]
+    w = torch.arange(n, dtype=torch.float32, device="cuda").view(1, n)       # the last half is kept
+    kept, out = torch.empty(1, **I32), torch.empty((1, n), device="cuda")
+    ws = torch.empty(sg.evict_workspace_size(1, 1, n), dtype=torch.uint8, device="cuda")
+    sg.sg_evict(t[0], t[1], cu([[rows - n]]), cu([n]), n, cu([k]), w, kept, out, ws, s_pool=t[2].view(rows, 2, 4))
+    assert kept.item() == k
+    for i, x in enumerate(t):
+        got = x[-n:].cpu().numpy()
+        assert (got[:k] == (np.arange(k, n) + 10 * i + 1)[:, None]).all()
+        assert not x[:-n].any()
+    assert np.array_equal(out[0, :k].cpu().numpy(), np.arange(k, n)) and not out[0, k:].any()
+
+
 def test_evict_bad_pages():
     """Rows outside the pool are ranked like any other; a move that touches one copies nothing."""
     say("evict bad pages")
