@@ -557,7 +557,7 @@ int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows
  *   v_pool, s_pool as above), any 1 <= G <= 16; dt is the type of q.  The
  *   stored values are used exactly and sums are fp32, so out differs from
  *   attention over the values in fp32 by fp32 rounding only.  weight_out may be
- *   NULL (then weight_in too): attention alone.
+ *   NULL (then weight_in too): attention alone.  scale: positive, at most 2e38.
  * A NaN row makes the outputs and weights of its unit NaN.
  *   ws      device workspace of at least the matching size, 16-byte aligned
  *           (with weights, 4 bytes per q head and row for the logits; split

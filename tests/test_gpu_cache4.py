@@ -497,3 +497,33 @@ def test_refused_where_it_would_not_fit():
                               torch.zeros((64, 128), dtype=torch.bfloat16, device="cuda"), table, n, 16, out,
                               torch.zeros((1, 2, c.table.shape[2] * 16), device="cuda"),
                               torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("pool", ["fp4", "bf16"])
+def test_table_far_longer_than_the_set(pool):
+    """A page table of 41 million rows (more chunks of weights than a launch has
+    workgroups in y) over a set of a thousand."""
+    say("long table", pool)
+    page, pages, n, d = 1 << 20, 40, 1000, 64
+    r = np.random.default_rng(2)
+    k, v = (r.standard_normal((n, d)).astype(np.float32) for _ in range(2))
+    q = torch.tensor(r.standard_normal((1, 1, d)), dtype=torch.float32).to(torch.bfloat16).cuda()
+    table, rows = torch.zeros((1, 1, pages), dtype=torch.int32, device="cuda"), page * pages
+    w, out = torch.full((1, 1, rows), 7.0, device="cuda"), torch.empty((1, 1, d), device="cuda")
+    if pool == "fp4":
+        (k4, sk), (v4, sv) = ref.encode(k), ref.encode(v)
+        k, v = ref.decode(k4, sk), ref.decode(v4, sv)
+        ws = torch.empty(sg.decode_fp4_workspace_size(1, 1, 1, d, pages, page, weights=True), dtype=torch.uint8,
+                         device="cuda")
+        sg.sg_decode_attn_fp4(q, torch.from_numpy(k4).cuda(), torch.from_numpy(v4).cuda(),
+                              torch.from_numpy(np.stack([sk, sv], axis=1)).cuda(), table, cu([[n]]), page, out, ws=ws,
+                              weight_out=w)
+    else:
+        kt, vt = (torch.from_numpy(x).to(torch.bfloat16).cuda() for x in (k, v))
+        k, v = kt.double().cpu().numpy(), vt.double().cpu().numpy()
+        ws = torch.empty(sg.decode_acc_workspace_size(1, 1, 1, d, pages, page), dtype=torch.uint8, device="cuda")
+        sg.sg_decode_attn_acc(q, kt, vt, table, cu([[n]]), page, out, w, ws)
+    want, tol, ww, wtol = ref.attention(q.double().cpu().numpy(), k, v, np.zeros((1, 1, pages), np.int32),
+                                        np.array([[n]]), page, d ** -0.5)
+    assert (np.abs(out.cpu().numpy() - want) <= tol).all()
+    assert (np.abs(w[0, 0, :n].cpu().numpy() - ww[0, 0]) <= wtol[0, 0]).all() and (w[0, 0, n:] == 7.0).all()
