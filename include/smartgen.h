@@ -558,7 +558,9 @@ int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows
  *   stored values are used exactly and sums are fp32, so out differs from
  *   attention over the values in fp32 by fp32 rounding only.  weight_out may be
  *   NULL (then weight_in too): attention alone.  scale: positive, at most 2e38.
- * A NaN row makes the outputs and weights of its unit NaN.
+ * A NaN key makes the outputs and weights of its unit NaN, a NaN value the
+ * outputs of its channel (SG_FP4: of its 32 channels); a set whose logits are
+ * all -inf gives zeros, as one without rows does.
  *   ws      device workspace of at least the matching size, 16-byte aligned
  *           (with weights, 4 bytes per q head and row for the logits; split
  *           states); no initialisation needed, calls that share one must be
