@@ -169,21 +169,25 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
     auto rows_of_unit = [&](int u) { return (int)max<int64_t>(0, min<int64_t>((int64_t)scalar_load(a.n_rows + u), max_rows)); };
     auto tiles_of = [](int n) { return (n + D4_TILE - 1) / D4_TILE; };
     Cursor4 cur{(int)blockIdx.x, 0, 0, 0};
-    int near = 0, n_near = 0, window = 64;   // lane i < window: rows of unit near + i
+    int near = 0, n_near = 0;                // lane i: rows of unit near + i
     if constexpr (SHARED) {
-        // The tile this share starts with: lane t sums the tiles of units
-        // [t * per, (t + 1) * per); the lane whose range holds it, then the unit.
+        // The tile this share starts with: lane i sums the tiles of units [64 i,
+        // 64 i + 64), read whole lines at a time (strided, a lane's units side by
+        // side, 2,048 units took 6 to 8 us longer); the lane whose 64 hold it,
+        // then the unit.
         const int per = (a.units + 63) / 64;         // at most 64
         int mine = 0, first8[8];
         auto rows8 = [&](int i0, int (&n)[8]) {
-            int c[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = a.n_rows[min(lane * per + i0 + i, a.units - 1)];
+            for (int i = 0; i < 8; ++i) n[i] = a.n_rows[min((i0 + i) * 64 + lane, a.units - 1)];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = i0 + i < per && lane * per + i0 + i < a.units;
-                n[i] = in ? (int)max<int64_t>(0, min<int64_t>(c[i], max_rows)) : 0;
-                mine += tiles_of(n[i]);
+                const bool in = (i0 + i) * 64 + lane < a.units;
+                n[i] = in ? (int)max<int64_t>(0, min<int64_t>(n[i], max_rows)) : 0;
+                if (i0 + i < per) {          // uniform
+                    const int sum = __builtin_amdgcn_readlane(wave_scan_incl(tiles_of(n[i])), 63);
+                    mine = lane == i0 + i ? sum : mine;
+                }
             }
         };
         rows8(0, first8);
@@ -205,15 +209,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
         const int p0 = share * each + min(share, more), p1 = p0 + each + (share < more ? 1 : 0);
         const int at = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < upto)) - 1);
         const int before = __builtin_amdgcn_readlane(upto - mine, at);
-        near = at * per;
-        if (per <= 8) {                      // the lane that sums them has them
-            window = per;
+        near = at * 64;
+        if (at < 8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) n_near = lane == i ? __builtin_amdgcn_readlane(first8[i], at) : n_near;
+            for (int i = 0; i < 8; ++i) n_near = at == i ? first8[i] : n_near;
         } else {
             n_near = near + lane < a.units ? rows_of(near + lane) : 0;
         }
-        const int t = lane < per ? tiles_of(n_near) : 0;
+        const int t = tiles_of(n_near);
         const int end = before + wave_scan_incl(t);
         const int i = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(p0 < end)) - 1);
         cur.unit = near + i;
@@ -230,7 +233,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
         c.tile = 0;
         do {
             ++c.unit;                        // tiles are left, so units with rows are
-            c.n = c.unit - near < window ? __builtin_amdgcn_readlane(n_near, c.unit - near) : rows_of_unit(c.unit);
+            c.n = c.unit - near < 64 ? __builtin_amdgcn_readlane(n_near, c.unit - near) : rows_of_unit(c.unit);
         } while (c.n == 0);
     };
 
@@ -448,123 +451,123 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
             advance(ents);
         }
         const int slot = st % NS;
-                        const char *sb = ring + slot * L::SLOT;
-                        const uint8_t *sc = reinterpret_cast<const uint8_t *>(sb + 2 * L::CODES);
-                        // bit i: row i of the tile counts
+        const char *sb = ring + slot * L::SLOT;
+        const uint8_t *sc = reinterpret_cast<const uint8_t *>(sb + 2 * L::CODES);
+        // bit i: row i of the tile counts
         const uint32_t live = (full >> slot) & 1u ? 0xffffffffu : (uint32_t)__ballot((valid >> slot) & 1u);
-                        // logits: lane (n16, kg) of half u gets rows 16 u + 4 kg + i of head n16
-                        float z[8];
+        // logits: lane (n16, kg) of half u gets rows 16 u + 4 kg + i of head n16
+        float z[8];
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const int row = 16 * u + n16;
-                            uint32_t kw[STEPS];
-                            uint32_t byte;
-                            if constexpr (D == 128) {
-                                const v4u x = *reinterpret_cast<const v4u *>(sb + row * 64 + ((kg ^ (n16 / 4)) * 16));
+        for (int u = 0; u < 2; ++u) {
+            const int row = 16 * u + n16;
+            uint32_t kw[STEPS];
+            uint32_t byte;
+            if constexpr (D == 128) {
+                const v4u x = *reinterpret_cast<const v4u *>(sb + row * 64 + ((kg ^ (n16 / 4)) * 16));
 #pragma unroll
-                                for (int s = 0; s < STEPS; ++s) kw[s] = x[s];
-                                byte = sc[row * SB + kg];
-                            } else {
-                                const uint2 x = *reinterpret_cast<const uint2 *>(sb + row * 32 + kg * 8);
-                                kw[0] = x.x;
-                                kw[1] = x.y;
-                                byte = sc[row * SB + kg / 2];
-                            }
-                            const float ks = fp4_scale(byte);
-                            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                for (int s = 0; s < STEPS; ++s) kw[s] = x[s];
+                byte = sc[row * SB + kg];
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2 *>(sb + row * 32 + kg * 8);
+                kw[0] = x.x;
+                kw[1] = x.y;
+                byte = sc[row * SB + kg / 2];
+            }
+            const float ks = fp4_scale(byte);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int s = 0; s < STEPS; ++s) {
-                                const bf16x8 kf = as_bf16x8(v4u{fp4_bf16_pair<0>(kw[s], ks), fp4_bf16_pair<1>(kw[s], ks),
-                                                                fp4_bf16_pair<2>(kw[s], ks), fp4_bf16_pair<3>(kw[s], ks)});
+            for (int s = 0; s < STEPS; ++s) {
+                const bf16x8 kf = as_bf16x8(v4u{fp4_bf16_pair<0>(kw[s], ks), fp4_bf16_pair<1>(kw[s], ks),
+                                                fp4_bf16_pair<2>(kw[s], ks), fp4_bf16_pair<3>(kw[s], ks)});
 #pragma unroll
-                                for (int p = 0; p < PARTS; ++p)
-                                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][s], acc, 0, 0, 0);
-                            }
+                for (int p = 0; p < PARTS; ++p)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[p][s], acc, 0, 0, 0);
+            }
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i];         // unscaled
-                        }
-                        if (live != 0xffffffffu) {
+            for (int i = 0; i < 4; ++i) z[4 * u + i] = acc[i];         // unscaled
+        }
+        if (live != 0xffffffffu) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                z[i] = (live >> (16 * (i / 4) + 4 * kg + i % 4)) & 1u ? z[i] : -INFINITY;
-                        }
-                        if constexpr (KEEP) {
-                            if (n16 < G) {
-                                float *zp = a.z + ((int64_t)cur.unit * G + n16) * a.z_stride + (int64_t)cur.tile * D4_TILE + 4 * kg;
+            for (int i = 0; i < 8; ++i)
+                z[i] = (live >> (16 * (i / 4) + 4 * kg + i % 4)) & 1u ? z[i] : -INFINITY;
+        }
+        if constexpr (KEEP) {
+            if (n16 < G) {
+                float *zp = a.z + ((int64_t)cur.unit * G + n16) * a.z_stride + (int64_t)cur.tile * D4_TILE + 4 * kg;
 #pragma unroll
-                                for (int u = 0; u < 2; ++u)
-                                    *reinterpret_cast<float4 *>(zp + 16 * u) =
-                                        make_float4(z[4 * u] * a.scale_log2, z[4 * u + 1] * a.scale_log2, z[4 * u + 2] * a.scale_log2,
+                for (int u = 0; u < 2; ++u)
+                    *reinterpret_cast<float4 *>(zp + 16 * u) =
+                        make_float4(z[4 * u] * a.scale_log2, z[4 * u + 1] * a.scale_log2, z[4 * u + 2] * a.scale_log2,
                                     z[4 * u + 3] * a.scale_log2);
-                            }
-                        }
-                        float top = z[0];
+            }
+        }
+        float top = z[0];
 #pragma unroll
-                        for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
         top *= a.scale_log2;
-                        if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
-                            top = fmaxf(top, __shfl_xor(top, 16, 64));
-                            top = fmaxf(top, __shfl_xor(top, 32, 64));
-                            const float mn = fmaxf(m, top);
-                            const float f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-                            l *= f;
-                            m = mn;
+        if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float mn = fmaxf(m, top);
+            const float f = mn == m ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+            l *= f;
+            m = mn;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float fi = __shfl(f, 4 * kg + i, 64);
+            for (int i = 0; i < 4; ++i) {
+                const float fi = __shfl(f, 4 * kg + i, 64);
 #pragma unroll
-                                for (int j = 0; j < NC; ++j) o[j][i] *= fi;
-                            }
-                        }
-                        const float ref = m == -INFINITY ? 0.f : m;
-                        uint32_t pw[3][8];
+                for (int j = 0; j < NC; ++j) o[j][i] *= fi;
+            }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        uint32_t pw[3][8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale_log2, -ref));
-                            l += p;
-                            uint32_t x[3];
-                            split3(p, x);
+        for (int i = 0; i < 8; ++i) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale_log2, -ref));
+            l += p;
+            uint32_t x[3];
+            split3(p, x);
 #pragma unroll
-                            for (int k = 0; k < 3; ++k) pw[k][i] = x[k];
-                        }
-                        bf16x8 pf[3];
+            for (int k = 0; k < 3; ++k) pw[k][i] = x[k];
+        }
+        bf16x8 pf[3];
 #pragma unroll
-                        for (int k = 0; k < 3; ++k)
-                            pf[k] = as_bf16x8(v4u{high_halves(pw[k][0], pw[k][1]), high_halves(pw[k][2], pw[k][3]),
-                                                  high_halves(pw[k][4], pw[k][5]), high_halves(pw[k][6], pw[k][7])});
-                        // values: 8 rows x NC channels per lane, as bf16 pairs of channels, then of rows
-                        uint32_t vb[8][NC / 2];
+        for (int k = 0; k < 3; ++k)
+            pf[k] = as_bf16x8(v4u{high_halves(pw[k][0], pw[k][1]), high_halves(pw[k][2], pw[k][3]),
+                                  high_halves(pw[k][4], pw[k][5]), high_halves(pw[k][6], pw[k][7])});
+        // values: 8 rows x NC channels per lane, as bf16 pairs of channels, then of rows
+        uint32_t vb[8][NC / 2];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int place = 16 * (i / 4) + 4 * (i % 4) + kg, row = 16 * (i / 4) + 4 * kg + i % 4;
-                            const char *vp = sb + L::CODES + place * (D / 2);
-                            uint32_t byte = sc[row * SB + SB / 2 + n16 * NC / FP4_BLOCK];
-                            // a row that is left out stands on pool row 0: its zero
-                            // probability must not meet a NaN
-                            if (live != 0xffffffffu) byte = (live >> row) & 1u ? byte : 0u;
-                            const float vs = fp4_scale(byte);
-                            uint32_t w;
-                            if constexpr (NC == 8) w = *reinterpret_cast<const uint32_t *>(vp + n16 * 4);
-                            else w = *reinterpret_cast<const uint16_t *>(vp + n16 * 2);
-                            vb[i][0] = fp4_bf16_pair<0>(w, vs);
-                            vb[i][1] = fp4_bf16_pair<1>(w, vs);
-                            if constexpr (NC == 8) {
-                                vb[i][2] = fp4_bf16_pair<2>(w, vs);
-                                vb[i][3] = fp4_bf16_pair<3>(w, vs);
-                            }
-                        }
+        for (int i = 0; i < 8; ++i) {
+            const int place = 16 * (i / 4) + 4 * (i % 4) + kg, row = 16 * (i / 4) + 4 * kg + i % 4;
+            const char *vp = sb + L::CODES + place * (D / 2);
+            uint32_t byte = sc[row * SB + SB / 2 + n16 * NC / FP4_BLOCK];
+            // a row that is left out stands on pool row 0: its zero
+            // probability must not meet a NaN
+            if (live != 0xffffffffu) byte = (live >> row) & 1u ? byte : 0u;
+            const float vs = fp4_scale(byte);
+            uint32_t w;
+            if constexpr (NC == 8) w = *reinterpret_cast<const uint32_t *>(vp + n16 * 4);
+            else w = *reinterpret_cast<const uint16_t *>(vp + n16 * 2);
+            vb[i][0] = fp4_bf16_pair<0>(w, vs);
+            vb[i][1] = fp4_bf16_pair<1>(w, vs);
+            if constexpr (NC == 8) {
+                vb[i][2] = fp4_bf16_pair<2>(w, vs);
+                vb[i][3] = fp4_bf16_pair<3>(w, vs);
+            }
+        }
 #pragma unroll
-                        for (int j = 0; j < NC; ++j) {
-                            v4u w;
+        for (int j = 0; j < NC; ++j) {
+            v4u w;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                w[i] = j % 2 == 0 ? low_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2])
-                                  : high_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2]);
+            for (int i = 0; i < 4; ++i)
+                w[i] = j % 2 == 0 ? low_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2])
+                                    : high_halves(vb[2 * i][j / 2], vb[2 * i + 1][j / 2]);
             const bf16x8 vf = as_bf16x8(w);
 #pragma unroll
-                            for (int k = 0; k < 3; ++k)
-                                o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[k], vf, o[j], 0, 0, 0);
-                        }
+            for (int k = 0; k < 3; ++k)
+                o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[k], vf, o[j], 0, 0, 0);
+        }
         const int unit = cur.unit;
         const bool last = (cur.tile + 1) * D4_TILE >= cur.n;
         advance(cur);
@@ -579,12 +582,22 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
     wait_vmem<0>();                          // nothing is under way to the LDS of whoever runs here next
 }
 
-// Whether wavefronts share the tiles of all units: where a unit could be cut,
-// the units are not too many for the lookup (64 per lane, more than the chip
-// holds wavefronts) and the tiles can be counted in 31 bits.
-static bool shares_tiles(int64_t units, int64_t max_rows) {
-    return max_rows > D4_MIN_SHARE * D4_TILE && units <= D4_SHARED_UNITS &&
-           units * ceil_div(max_rows, D4_TILE) <= 0x7fffffffll;
+// Whether wavefronts share the tiles of all units: where the units are long, not
+// too many for the lookup (64 per lane, more than the chip holds wavefronts), and
+// the tiles can be counted in 31 bits.  One wavefront per short unit costs neither
+// the lookup nor, without weights, the launch that joins states; a long one keeps
+// its wavefront busy behind the others.  In us, shared / a wavefront per unit
+// (d = 128, G = 4, bf16 queries, all units with table room for max_rows rows):
+//   8 units     128 rows 12.4 / 9.6    256 rows 12.8 / 12.3    512 rows 12.2 / 21.6
+//   512 units   128 rows 13.5 / 9.5    256 rows 15.9 / 13.0    512 rows 20.9 / 22.9
+//   1,024       128 rows 18.1 / 9.5    256 rows 23.7 / 13.3    512 rows 29.0 / 23.3
+//   2,048       128 rows 28.6 / 11.9   256 rows 35.4 / 19.3    512 rows 46.8 / 33.2
+//   2,048       256 to 2,048 rows 77 / 106
+//   with weights (1 to max_rows rows): 8 units of 128 rows 13.5 / 13.6, of 256
+//   rows 13.3 / 17.0; 1,024 units of 128 rows 19.6 / 17.6, of 256 rows 22.8 / 24.2
+static bool shares_tiles(int64_t units, int64_t max_rows, bool weights) {
+    const int64_t whole = weights ? 128 : units >= 1024 ? 512 : 256;
+    return max_rows > whole && units <= D4_SHARED_UNITS && units * ceil_div(max_rows, D4_TILE) <= 0x7fffffffll;
 }
 // Wavefronts that share them (the kernel uses fewer where the units are short).
 template <typename T>
@@ -596,7 +609,7 @@ struct Decode4Sizes {      // bytes of the workspace's parts (for either type of
     size_t z, states, spans;
 };
 static Decode4Sizes decode4_sizes(int64_t units, int G, int d, int64_t max_rows, bool weights) {
-    const bool shared = shares_tiles(units, max_rows);
+    const bool shared = shares_tiles(units, max_rows, weights);
     const size_t slots = shared ? (size_t)(units + shared_waves<uint16_t>(units, max_rows)) : weights ? (size_t)units : 0;
     return {weights ? (size_t)units * G * z_stride_of(max_rows) * sizeof(float) : 0,
             slots * G * (size_t)(d + 2) * sizeof(float), shared ? (size_t)units * sizeof(int2) : 0};
@@ -606,7 +619,7 @@ template <typename T, int D>
 static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, Weights w, char *ws, size_t ws_bytes) {
     const int G = a.Hq / a.Hkv;
     const int64_t units = (int64_t)B * a.Hkv, max_rows = (int64_t)a.max_pages * a.page_size;
-    const bool weights = w.out != nullptr, shared = shares_tiles(units, max_rows);
+    const bool weights = w.out != nullptr, shared = shares_tiles(units, max_rows, weights);
     const Decode4Sizes sz = decode4_sizes(units, G, D, max_rows, weights);
     const size_t need = sz.z + sz.states + sz.spans;
     SG_REQUIRE(need <= ws_bytes && (need == 0 || ws), SG_EWORKSPACE, "%s: needs %zu bytes of workspace, %zu given", fn,

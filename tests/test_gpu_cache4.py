@@ -445,6 +445,34 @@ def test_attention_short_units_in_a_row(page):
     c.check(None, 1.0, True)
 
 
+@pytest.mark.parametrize("units,page,d,dtype", [(8, 16, 128, "bf16"), (600, 24, 64, "bf16"), (2050, 16, 128, "f32"),
+                                                (4096, 10, 64, "bf16")])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_short_units_of_long_tables(units, page, d, dtype, weights):
+    """Tables with room for far more rows than any unit has, as a cache has them
+    early on: units without a row and shorter than a tile among them."""
+    say("short units of long tables", units, page, d, dtype, weights)
+    r = np.random.default_rng(units + 1)
+    lens = np.where(r.random(units // 2) < 0.3, 0, r.integers(1, 70, units // 2))
+    lens[2:2 + units // 8] = 0                          # a run of empty ones
+    c = Case(lens.tolist(), 4, 2, d, page, dtype, "fp4", seed=units, extra_pages=0)
+    c.table = np.pad(c.table, ((0, 0), (0, 0), (0, -(-800 // page))))
+    a = c.check(None, 1.0, weights)
+    assert np.array_equal(a[0], c.run(None, 1.0, weights)[0])
+
+
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_lengths_around_the_plans(weights):
+    """Tables on either side of the capacities at which the launch changes, sets of
+    nothing up to a full table: the same definition holds."""
+    say("tables around the plans", weights)
+    for units in (4, 1024):
+        for pages in (8, 9, 16, 17, 32, 33):
+            lens = [(16 * pages * (i % 5)) // 4 for i in range(units // 2)]
+            c = Case(lens, 2, 2, 64, 16, "bf16", "fp4", seed=pages, extra_pages=0)
+            c.check(None, 1.0, weights)
+
+
 def test_outputs_at_any_float():
     say("outputs at any float")
     for pool in ("fp4", "bf16"):
