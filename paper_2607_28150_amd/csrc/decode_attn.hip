@@ -119,6 +119,11 @@ __device__ __forceinline__ float *part_ptr(float *ws, int64_t unit, int nsplit, 
     return ws + ((unit * nsplit + split) * G) * (int64_t)(d + 2);
 }
 
+// What the V loads of a row that is left out read: its probability is 0, and
+// 0 times a NaN or an infinity of whatever row stood there would be NaN.  (Its
+// K loads may read any row: the logit is replaced by -inf.)
+static __device__ const v4u zero_row[128 * sizeof(float) / sizeof(v4u)] = {};
+
 // DPP lane moves (gfx9 encodings): quad_perm, row rotate, row half-mirror
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
@@ -319,27 +324,35 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
     }
 
     // pool row of logical row lr, or -1 (past the range or outside the pool).
-    // rel < npg * page_size <= max_rows <= 2^30, and rel / page_size is the
-    // exact multiply-shift (rel * page_mul) >> page_shift set up by the host
-    auto pool_row = [&](int64_t lr) -> int {
-        const uint32_t rel = (uint32_t)(min<int64_t>(lr, w1 - 1) - pg0 * page_size);
-        const uint32_t pi = (uint32_t)(((uint64_t)rel * page_mul) >> page_shift);
-        const int64_t x = (int64_t)pte[pi] + (int)(rel - pi * (uint32_t)page_size);
-        return (lr < w1 && x >= 0 && x < pool_rows) ? (int)x : -1;
+    // Rows and pool rows fit 32 bits: rel < npg * page_size <= max_rows <= 2^30,
+    // rel / page_size is the exact multiply-shift (rel * page_mul) >> page_shift
+    // set up by the host, and a page entry plus a place in its page, taken as
+    // unsigned, is below pool_rows < 2^31 only where it is so as a signed sum.
+    const uint32_t rel_end = (uint32_t)(w1 - pg0 * page_size), pool_end = (uint32_t)pool_rows;
+    auto pool_row = [&](uint32_t rel) -> int {
+        const uint32_t in = min(rel, rel_end - 1u);
+        const uint32_t pi = (uint32_t)(((uint64_t)in * page_mul) >> page_shift);
+        const uint32_t x = (uint32_t)pte[pi] + (in - pi * (uint32_t)page_size);
+        return rel < rel_end && x < pool_end ? (int)x : -1;
     };
     char *myring = ring + wave * (NS * SLOTB);
-    // the loads of the step at row t into ring slot `slot`: vector j * LPR + c
+    // the loads of step `step` into ring slot `slot`: vector j * LPR + c
     // of the lane's row lands at slot + j KB + 16 lane.  A row left out reads
-    // pool row 0 (in bounds: the pool is not empty when a wavefront has rows;
-    // the repeated address stays in L2) and its bit in `valid` clears.
-    auto issue = [&](int64_t t, int slot, unsigned &valid) {
+    // K of pool row 0 (in bounds: the pool is not empty when a wavefront has
+    // rows) and V of zero_row, repeated addresses that stay in L2, and its bit
+    // in `valid` clears.  (Cheaper than zeros put in the place of its values
+    // later: 16 fp32 requests with 4 heads per KV head 62.2 us, with a test for
+    // such rows at every step 66.9.)
+    const uint32_t rel0 = (uint32_t)(w0 - pg0 * page_size) + r;      // this lane's row of step 0
+    auto issue = [&](int step, int slot, unsigned &valid) {
         char *sb = myring + slot * SLOTB;
-        const int pr = pool_row(t + r);
+        const int pr = pool_row(rel0 + (uint32_t)step * RPS);
         const int64_t off = (int64_t)max(pr, 0) * CPR + c;
+        const v4u *vr = pr >= 0 ? v_pool + off : zero_row + c;
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             dma16_nt(k_pool + off + j * LPR, lds_addr(sb + j * 1024));
-            dma16_nt(v_pool + off + j * LPR, lds_addr(sb + STEPB + j * 1024));
+            dma16_nt(vr + j * LPR, lds_addr(sb + STEPB + j * 1024));
         }
         valid = (valid & ~(1u << slot)) | ((pr >= 0 ? 1u : 0u) << slot);
     };
@@ -489,7 +502,7 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         const int nst = (int)ceil_div(w1 - w0, RPS);
         unsigned valid = 0u;
 #pragma unroll
-        for (int s = 0; s < NS - 1; ++s) issue(w0 + (int64_t)s * RPS, s, valid);
+        for (int s = 0; s < NS - 1; ++s) issue(s, s, valid);
         // The hot loop has no rescale in it (a rescale inside makes the
         // compiler copy every accumulator each step): a step whose logits
         // would pass the reference leaves the loop, is rescaled and
@@ -499,9 +512,9 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         for (;;) {
             bool grew = false;
             for (; i < nst; ++i) {
-                // past the range these loads read pool row 0 (kept uniform so
-                // the wait below is a constant)
-                issue(w0 + (int64_t)(i + NS - 1) * RPS, (i + NS - 1) % NS, valid);
+                // past the range these loads read rows that are left out (kept
+                // uniform so the wait below is a constant)
+                issue(i + NS - 1, (i + NS - 1) % NS, valid);
                 wait_vmem<(NS - 1) * 2 * VPL>();          // step i has landed
                 const char *sb = myring + (i % NS) * SLOTB;
                 const bool raise = logits(sb, (valid >> (i % NS)) & 1u, z);
