@@ -566,6 +566,9 @@ int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows
  *           states); no initialisation needed, calls that share one must be
  *           ordered.  `weights` of the size call:
  *           whether weight_out is given.
+ * Units (B * Hkv) beyond what a launch can hold, 2^32 - 1 threads with 256 per
+ * unit (SG_FP4: 64, with weights 128), or 1,024 where a unit is cut into
+ * hundreds of states, are refused with SG_EUNSUPPORTED.
  */
 size_t sg_decode_attn_acc_workspace_size(int B, int Hq, int Hkv, int d, int max_pages, int page_size);
 int sg_decode_attn_acc(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d, float scale, const void *q,

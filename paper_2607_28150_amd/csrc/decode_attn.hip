@@ -788,6 +788,9 @@ static int launch_decode(const char *fn, hipStream_t s, int B, int Hq, int Hkv, 
         set_error("%s: %lld splits of %lld rows are not supported", fn, (long long)nsplit, (long long)split_rows);
         return SG_EUNSUPPORTED;
     }
+    SG_REQUIRE((parts || units <= max_workgroups(64 * WAVES)) &&
+                   (!acc || units <= max_workgroups(finish_threads(D, nsplit))),
+               SG_EUNSUPPORTED, "%s: too many units", fn);
     const size_t zfloats = acc ? (size_t)units * G * z_stride_of(max_rows) : 0;
     const size_t need = (acc || nsplit > 1 ? (size_t)units * nsplit * G * (D + 2) * sizeof(float) : 0) +
                         zfloats * sizeof(float);

@@ -620,6 +620,10 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     const int G = a.Hq / a.Hkv;
     const int64_t units = (int64_t)B * a.Hkv, max_rows = (int64_t)a.max_pages * a.page_size;
     const bool weights = w.out != nullptr, shared = shares_tiles(units, max_rows, weights);
+    const unsigned grid = shared ? (unsigned)shared_waves<T>(units, max_rows) : (unsigned)units;
+    const int64_t expect = shared ? grid / units + 1 : 1;      // states per unit
+    SG_REQUIRE(!(weights || shared) || units <= max_workgroups(finish_threads(D, expect)), SG_EUNSUPPORTED,
+               "%s: too many units", fn);
     const Decode4Sizes sz = decode4_sizes(units, G, D, max_rows, weights);
     const size_t need = sz.z + sz.states + sz.spans;
     SG_REQUIRE(need <= ws_bytes && (need == 0 || ws), SG_EWORKSPACE, "%s: needs %zu bytes of workspace, %zu given", fn,
@@ -629,7 +633,6 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     a.z_stride = w.z_stride = z_stride_of(max_rows);
     a.spans = shared ? reinterpret_cast<int2 *>(ws + sz.z) : nullptr;
     a.states = reinterpret_cast<float *>(ws + sz.z + sz.spans);
-    const unsigned grid = shared ? (unsigned)shared_waves<T>(units, max_rows) : (unsigned)units;
     const bool halves = a.page_size % 16 == 0;
 #define SG_D4(KEEP, SHARED)                                                           \
     do {                                                                              \
@@ -642,7 +645,7 @@ static int launch_decode4(const char *fn, hipStream_t s, int B, Decode4Args a, W
     else SG_D4(false, false);
 #undef SG_D4
     if (weights || shared)
-        launch_finish<D>(s, units, G, shared ? grid / units + 1 : 1, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
+        launch_finish<D>(s, units, G, expect, 1, a.n_rows, max_rows, 0, a.spans, a.states, a.out, w);
     return launch_status(fn);
 }
 

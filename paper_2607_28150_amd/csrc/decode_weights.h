@@ -160,9 +160,15 @@ static __global__ __launch_bounds__(THREADS) void decode_finish_kernel(
     }
 }
 
-// `expect`: states per unit.  As many threads as take them in one go, eight
-// each: a block of 1,024 threads for a head's few hundred, of 128 where every
-// unit has a handful and the heads fill the chip.
+// Threads of a block that joins about `expect` states per unit: eight states
+// each in one go, a block of 1,024 threads for a head's few hundred, of 128
+// where every unit has a handful and the heads fill the chip.  (`expect` is a
+// mean: where lengths differ much, a long unit's states take more rounds.)
+inline int finish_threads(int d, int64_t expect) {
+    const int64_t threads = ceil_div(expect, 8) * d;
+    return threads <= 128 ? 128 : threads <= 256 ? 256 : threads <= 512 ? 512 : 1024;
+}
+
 template <int D>
 static void launch_finish(hipStream_t s, int64_t units, int G, int64_t expect, int nsplit, const int32_t *n_rows,
                           int64_t max_rows, int64_t split_rows, const int2 *spans, const float *states, float *out,
@@ -173,11 +179,12 @@ static void launch_finish(hipStream_t s, int64_t units, int G, int64_t expect, i
         const dim3 grid((unsigned)units, (unsigned)(G + chunks));
         kernel<<<grid, threads, 0, s>>>(G, nsplit, n_rows, max_rows, split_rows, spans, states, out, w);
     };
-    const int64_t threads = ceil_div(expect, 8) * D;
-    if (threads <= 128) launch(decode_finish_kernel<D, 128>, 128);
-    else if (threads <= 256) launch(decode_finish_kernel<D, 256>, 256);
-    else if (threads <= 512) launch(decode_finish_kernel<D, 512>, 512);
-    else launch(decode_finish_kernel<D, 1024>, 1024);
+    switch (finish_threads(D, expect)) {
+        case 128: return launch(decode_finish_kernel<D, 128>, 128);
+        case 256: return launch(decode_finish_kernel<D, 256>, 256);
+        case 512: return launch(decode_finish_kernel<D, 512>, 512);
+        default: return launch(decode_finish_kernel<D, 1024>, 1024);
+    }
 }
 
 }  // namespace sg
