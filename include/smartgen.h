@@ -613,7 +613,7 @@ int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d,
  *   n_kept, weight_out, pos_out  as n_rows, weight, pos; each may be its input
  *           (in place) and must not otherwise overlap it.  With outputs of
  *           their own, the same call made again writes the same results.
- *   sinks >= 0 (0: none); recent_from device int32 [units] or NULL (none).
+ *   sinks >= 0 (0: none, whatever the positions); recent_from device int32 [units] or NULL (none).
  *   ws      device workspace of at least sg_evict_workspace_size(...) bytes,
  *           16-byte aligned.
  * Requirements: max_pages * page_size <= 81920.

@@ -299,6 +299,7 @@ extern "C" int sg_evict(void *stream, sg_dtype dt, int units, int d, void *k_poo
     const size_t need = sg_evict_workspace_size(units, max_pages, page_size);
     SG_REQUIRE(ws && ws_bytes >= need, SG_EWORKSPACE, "%s: needs %zu bytes of workspace, %zu given", fn, need, ws_bytes);
     int2 *moves = reinterpret_cast<int2 *>(ws);
+    if (sinks == 0) sinks = INT32_MIN;      // no position is below it, negative ones neither
     const EvictArgs a{reinterpret_cast<v4u *>(k_pool), reinterpret_cast<v4u *>(v_pool), s_pool, pool_rows, page_table,
                       n_rows, page_size, max_pages, budget, weight, pos, stride, sinks, recent_from, n_kept, weight_out,
                       pos_out, moves, reinterpret_cast<int32_t *>(moves + (size_t)units * (cap / 2))};
