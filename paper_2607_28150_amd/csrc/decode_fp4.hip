@@ -95,6 +95,11 @@ __device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
     p[1] = __float_as_uint(r);
     p[2] = __float_as_uint(r - __uint_as_float(p[1] & 0xffff0000u));
 }
+// The same of a value that may be infinite, which its first part alone then is.
+__device__ __forceinline__ void split_query(float x, uint32_t (&p)[3]) {
+    split3(x, p);
+    if (fabsf(x) == INFINITY) p[1] = p[2] = 0u;
+}
 // The high halves of two words, or their low halves, as a pair.
 __device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 __device__ __forceinline__ uint32_t low_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100u); }
@@ -353,8 +358,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t c[3], e[3];
-                    split3(__uint_as_float(i < 2 ? x[2 * i] : y[2 * i - 4]), c);
-                    split3(__uint_as_float(i < 2 ? x[2 * i + 1] : y[2 * i - 3]), e);
+                    split_query(__uint_as_float(i < 2 ? x[2 * i] : y[2 * i - 4]), c);
+                    split_query(__uint_as_float(i < 2 ? x[2 * i + 1] : y[2 * i - 3]), e);
 #pragma unroll
                     for (int p = 0; p < 3; ++p) w[p][i] = high_halves(c[p], e[p]);
                 }
