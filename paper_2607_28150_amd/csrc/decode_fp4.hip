@@ -87,18 +87,13 @@ __device__ __forceinline__ bf16x8 as_bf16x8(const v4u &w) {
 }
 
 // x cut into three parts of 8 significant bits each, in the high halves of
-// p[0], p[1], p[2] (what the low halves hold does not count): their sum is x
-// (a part below the smallest normal is lost).
+// p[0], p[1], p[2] (what the low halves hold does not count): their sum is x,
+// less what lies below 2^-133, the least bf16.
 __device__ __forceinline__ void split3(float x, uint32_t (&p)[3]) {
     p[0] = __float_as_uint(x);
     const float r = x - __uint_as_float(p[0] & 0xffff0000u);
     p[1] = __float_as_uint(r);
     p[2] = __float_as_uint(r - __uint_as_float(p[1] & 0xffff0000u));
-}
-// The same of a value that may be infinite, which its first part alone then is.
-__device__ __forceinline__ void split_query(float x, uint32_t (&p)[3]) {
-    split3(x, p);
-    if (fabsf(x) == INFINITY) p[1] = p[2] = 0u;
 }
 // The high halves of two words, or their low halves, as a pair.
 __device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
@@ -344,28 +339,64 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
     float m, l;                              // of head n16 (l: this lane's rows)
     f32x4 o[NC];                             // o[j][i]: head 4 kg + i, channel NC n16 + j
     int begun = cur.tile;                    // first tile taken of the current unit
+    float scale = a.scale_log2;              // of head n16's logits
     auto begin_unit = [&](int unit) {
         const int b = unit / Hkv, h = unit % Hkv;
+        const T *qp = reinterpret_cast<const T *>(a.q) +
+                      ((int64_t)b * Hq + (int64_t)h * G + min(n16, G - 1)) * D + kg * (D / 4);
+        if constexpr (PARTS == 1) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const T *qp = reinterpret_cast<const T *>(a.q) +
-                          ((int64_t)b * Hq + (int64_t)h * G + min(n16, G - 1)) * D + kg * (D / 4) + s * 8;
-            v4u w[PARTS];
-            if constexpr (PARTS == 1) {
-                w[0] = *reinterpret_cast<const v4u *>(qp);
-            } else {
-                const v4u x = *reinterpret_cast<const v4u *>(qp), y = *reinterpret_cast<const v4u *>(qp + 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t c[3], e[3];
-                    split_query(__uint_as_float(i < 2 ? x[2 * i] : y[2 * i - 4]), c);
-                    split_query(__uint_as_float(i < 2 ? x[2 * i + 1] : y[2 * i - 3]), e);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) w[p][i] = high_halves(c[p], e[p]);
-                }
+            for (int s = 0; s < STEPS; ++s) {
+                const v4u w = *reinterpret_cast<const v4u *>(qp + s * 8);
+                qf[0][s] = as_bf16x8(n16 < G ? w : v4u{0u, 0u, 0u, 0u});
             }
+        } else {
+            float x[STEPS][8], top = 0.f;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) qf[p][s] = as_bf16x8(n16 < G ? w[p] : v4u{0u, 0u, 0u, 0u});
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const v4u w = *reinterpret_cast<const v4u *>(qp + s * 8 + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[s][i + j] = __uint_as_float(w[j]);
+                }
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[s][i]));
+            auto cut = [&](auto split) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    v4u w[PARTS];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t c[3], e[3];
+                        split(x[s][2 * i], c);
+                        split(x[s][2 * i + 1], e);
+#pragma unroll
+                        for (int p = 0; p < 3; ++p) w[p][i] = high_halves(c[p], e[p]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) qf[p][s] = as_bf16x8(n16 < G ? w[p] : v4u{0u, 0u, 0u, 0u});
+                }
+            };
+            scale = a.scale_log2;
+            if (__all(top >= 0x1p-60f && top < INFINITY)) {          // uniform
+                cut(split3);
+            } else {
+                // Parts below 2^-133 do not exist in bf16: a head of small values
+                // is taken 2^48 times, where the least bit of any float lies above
+                // that and 128 products with the largest key (6 * 2^125) stay
+                // finite.  An infinity is its first part alone.
+                const uint64_t large = __ballot(top >= 0x1p-60f);    // bit 16 kg + n16
+                const bool small = !(((large | large >> 16 | large >> 32 | large >> 48) >> n16) & 1u);
+                const float up = small ? 0x1p48f : 1.f;
+                if (small) scale *= 0x1p-48f;
+                cut([&](float v, uint32_t (&p)[3]) {
+                    split3(v * up, p);
+                    if (fabsf(v) == INFINITY) p[1] = p[2] = 0u;
+                });
+            }
         }
         // waited for here, once per unit: the compiler does not see the ring's
         // loads and would otherwise drain them at every step
@@ -502,14 +533,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
                     *reinterpret_cast<float4 *>(zp + 16 * u) =
-                        make_float4(z[4 * u] * a.scale_log2, z[4 * u + 1] * a.scale_log2, z[4 * u + 2] * a.scale_log2,
-                                    z[4 * u + 3] * a.scale_log2);
+                        make_float4(z[4 * u] * scale, z[4 * u + 1] * scale, z[4 * u + 2] * scale,
+                                    z[4 * u + 3] * scale);
             }
         }
         float top = z[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
-        top *= a.scale_log2;
+        top *= scale;
         if (__any(top > m + D4_LAZY)) {      // raise every head's reference (rare)
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -528,7 +559,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
         uint32_t pw[3][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale_log2, -ref));
+            const float p = __builtin_amdgcn_exp2f(fmaf(z[i], scale, -ref));
             l += p;
             uint32_t x[3];
             split3(p, x);

@@ -36,3 +36,18 @@ def test_infinite_query(dtype, d, sign):
     for (b, h), x in ww.items():
         if (b, h) != (1, 1):
             assert (np.abs(w[b, h, :len(x)] - x) <= wtol[b, h] + 1e-37).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size,byte", [(2.0 ** -59, 186), (2.0 ** -61, 188), (1e-30, 220), (1e-36, 247), (3e-38, 251),
+                                       (1e-38, 252), (1e-39, 252)])
+def test_tiny_queries(d, size, byte):
+    """Small fp32 queries (subnormal ones too) against large keys: logits of ordinary size, as
+    exact as any; one head of another size beside them."""
+    say("tiny queries", d, size, byte)
+    c = Case([40, 70, 0, 33], 3, 2, d, 16, "f32", "fp4", seed=d)
+    c.pools[2][:, 0] = byte
+    c.q.mul_(size)
+    c.q[1, 2] *= 2.0 ** -9
+    c.check(c.r.random((4, 2, c.table.shape[2] * 16)), 0.5)
+    c.check(None, 1.0, False)
