@@ -620,6 +620,7 @@ def _row_code(k, v, s, d, what):
 
 
 def _row_width(k):
+    _need(k.shape[-1] > 0, "rows without channels")
     return k.shape[-1] * (2 if k.dtype == torch.uint8 else 1)
 
 
@@ -670,6 +671,7 @@ def _decode_shape(q, page_table, n_rows, out, page_size, weight, weight_out):
     _need(page_table.dim() == 3 and page_table.shape[0] == B, "page_table must be [B][Hkv][max_pages]")
     Hkv, max_pages = page_table.shape[1], page_table.shape[2]
     _need(Hkv > 0 and Hq % Hkv == 0, "Hq must be a multiple of Hkv")
+    _need(d > 0, "queries without channels")
     _int32(page_table, 0, "page_table")
     _int32(n_rows, B * Hkv, "n_rows")
     _need(out.dtype == torch.float32 and out.numel() >= B * Hq * d, "out must be float32 [B][Hq][d]")
@@ -731,6 +733,7 @@ def sg_evict(k_pool, v_pool, page_table, n_rows, page_size, budget, weight, n_ke
     the new count move into the holes before it, with their weights and positions.
     n_kept, weight_out and pos_out may be n_rows, weight and pos."""
     max_pages = page_table.shape[-1]
+    _need(max_pages > 0, "page_table has room for no page")
     units = page_table.numel() // max_pages
     d = _row_width(k_pool)
     dt, pool_rows = _row_code(k_pool, v_pool, s_pool, d, "pool")

@@ -3,6 +3,7 @@ before anything is enqueued (no GPU needed)."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2607_28150_amd import smartgen as sg
 
@@ -38,3 +39,20 @@ def test_units_of_many_states(lib):
     rc = lib.sg_decode_attn_acc(None, 1, 5_000_000, 1, 1, 128, 0.1, P, P, P, 10, P, P, 1, 1 << 18, P, None, 1.0, P, 1 << 18,
                                 P, 1 << 62)
     assert rc == sg.SG_EUNSUPPORTED and "units" in lib.sg_last_error().decode()
+
+
+def test_binding_refuses_empty_axes():
+    """Rows of no channels and tables of no pages: ValueError, as for any other shape that does not fit."""
+    f, u8 = torch.zeros, (lambda *s: torch.zeros(s, dtype=torch.uint8))
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)  # noqa: E731
+    base = torch.zeros(1, dtype=torch.int64)
+    with pytest.raises(ValueError, match="channels"):
+        sg.sg_fetch_fp4(i32(2), 1, None, None, base, f(4, 0), f(4, 0), i32(1, 1), 16, i32(1), u8(4, 0), u8(4, 0),
+                        s_pool=u8(4, 2, 0))
+    for pools, s in ((f(4, 0), None), (u8(4, 0), u8(4, 2, 0))):
+        with pytest.raises(ValueError, match="channels"):
+            sg.sg_evict(pools, pools, i32(1, 2), i32(1), 16, i32(1), f(1, 32), i32(1), f(1, 32), None, s_pool=s)
+    with pytest.raises(ValueError, match="page"):
+        sg.sg_evict(f(4, 64), f(4, 64), i32(2, 0), i32(2), 16, i32(2), f(2, 32), i32(2), f(2, 32), None)
+    with pytest.raises(ValueError, match="channels"):
+        sg.sg_decode_attn_acc(f(1, 8, 0), f(4, 0), f(4, 0), i32(1, 8, 2), i32(1, 8), 16, f(1, 8, 0), f(1, 8, 32), None)
