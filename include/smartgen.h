@@ -512,7 +512,8 @@ int sg_spec_commit(void *stream, int L, int Hkv, int64_t T, int64_t s0, int64_t 
  *
  * A code is a sign (bit 3) over one of the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4,
  * 6 (E2M1); a scale byte e stands for 2^(e - 127), 255 for NaN (E8M0); a value
- * is code x scale, exact in bf16.  A row of d = 128 is 68 bytes (bf16: 256).
+ * is code x scale, exact in bf16 (bytes 253 and 254, which no call here makes,
+ * can pass its range).  A row of d = 128 is 68 bytes (bf16: 256).
  *
  * Storing a block of 32 channels with largest magnitude t: the scale is the
  * smallest 2^e with t <= 7 x 2^e (byte 2 at least, 252 at most), every channel
@@ -558,6 +559,9 @@ int sg_fetch_fp4(void *stream, sg_dtype src_dt, sg_dtype dst_dt, int d, int rows
  *   stored values are used exactly and sums are fp32, so out differs from
  *   attention over the values in fp32 by fp32 rounding only.  weight_out may be
  *   NULL (then weight_in too): attention alone.  scale: positive, at most 2e38.
+ * In all decode attention a probability is held to 2^-126 of its head's
+ * largest, and sums run over probabilities of up to 2^16 before they are
+ * divided: values up to 2^80 cannot overflow.
  * A NaN key makes the outputs and weights of its unit NaN, a NaN value the
  * outputs of its channel (SG_FP4: of its 32 channels); a set whose logits are
  * all -inf gives zeros, as one without rows does.
@@ -590,8 +594,9 @@ int sg_decode_attn_fp4(void *stream, sg_dtype dt, int B, int Hq, int Hkv, int d,
  *   - guarded rows first: those holding a token position below `sinks` or at or
  *     above recent_from[u] (position = pos[u][i], or i when pos is NULL);
  *   - then larger weight first;
- *   - equal weights, and guarded rows among themselves, by lower row; NaN ranks
- *     below every number.
+ *   - equal weights, and guarded rows among themselves, by lower row (a budget
+ *     below the number of guarded rows keeps the lower ones); NaN ranks below
+ *     every number.
  *
  * The order of a set's rows does not matter to attention (Section 4.2), so
  * only the holes are filled: the kept rows at and past k, in ascending order,

@@ -46,7 +46,9 @@
 // sg_decode_attn_acc is the same kernel with one store more per step, each
 // row's logits into the workspace, and a second launch that joins the splits
 // and turns the logits into weights (decode_weights.h) in the place of the merge:
-// 64 requests of 245 to 3,932 bf16 rows 121 + 10.7 us, 573 MB at 4.7 TB/s.
+// 64 requests of 245 to 3,932 bf16 rows 118.9 + 10.6 us, one of 819 rows 12.9 +
+// 3.9.  Without the logits the same rows take 95.3 + 4.8 and 8.0 + 3.5 us, so
+// their stores cost 24 us for 17 MB: far more than the bytes, see keep_logits.
 #include <mutex>
 
 #include "decode_weights.h"
@@ -401,8 +403,10 @@ __global__ __launch_bounds__((64 * DecodeShape<T, D, HG>::WAVES)) void decode_ke
         return __any(grow);
     };
     // the logits of row lr (this lane's) for the weights: lane c < HG of the row
-    // stores head c's.  The wait for the ring's loads counts loads alone, so a
-    // store in flight only makes it wait for more of them than it needs.
+    // stores head c's.  Stores count among the operations that the ring's wait
+    // leaves in flight, so it waits for no fewer loads than it needs, but with
+    // NS - 1 stores among them for some of the next step's as well; each also
+    // covers pieces of 16 or 32 bytes only.
     auto keep_logits = [&](int64_t lr, const float (&z)[HG]) {
         if constexpr (ACC) {
             const int gl0 = (int)blockIdx.z * HG;      // first head within the KV group

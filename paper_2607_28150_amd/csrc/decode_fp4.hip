@@ -36,12 +36,13 @@
 // fp32 queries and the probabilities are cut into three bf16 parts of 8 bits
 // that add up to them exactly, so nothing is rounded below fp32.
 //
-// Bound by memory where the work is large (16 prompts of 8K to 32K rows: 63 us
-// for 321 MB, 5.1 TB/s, above the rate of a device copy; the counters see every
-// byte read once), by start and end where it is not: a launch, the lookup, the
-// first rows' round trips and the states make up 10 of 36 us for 64 requests of
-// 148 MB, and nearly all of 7.1 us for one.  Vector instructions fill 44% of a
-// SIMD's cycles, matrix instructions 16%.
+// Bound by memory where the work is large (16 prompts of 8K to 32K rows: 68 us
+// for 321 MB, 4.7 TB/s, the rate of a device copy; whole calls differ by 7 us
+// from card to card; the counters see every byte read once), by start and end
+// where it is not: a launch, the lookup, the first rows' round trips and the
+// states are what 64 requests of 146 MB take beyond a copy's time, 6 of 36.5 us,
+// and nearly all of 7.2 us for one.  Vector instructions fill 47% of a SIMD's
+// cycles in the batch, matrix instructions 17%.
 //
 // Softmax as in sg_decode_attn: online in log2 units against a reference max
 // per head that is raised only when a logit passes it by 2^16.
@@ -620,7 +621,9 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(Plan4<T>::WA
 
 // Whether wavefronts share the tiles of all units: where the units are long, not
 // too many for the lookup (64 per lane, more than the chip holds wavefronts), and
-// the tiles can be counted in 31 bits.  One wavefront per short unit costs neither
+// the tiles can be counted in 31 bits.  Above the lookup's limit a long unit holds
+// up the rest: 4,096 units of which eight have 32,768 rows and the others 300 take
+// 75 us, 4,104 such 1,192 (300 rows each: 45).  One wavefront per short unit costs neither
 // the lookup nor, without weights, the launch that joins states; a long one keeps
 // its wavefront busy behind the others.  In us, shared / a wavefront per unit
 // (d = 128, G = 4, bf16 queries, all units with table room for max_rows rows):

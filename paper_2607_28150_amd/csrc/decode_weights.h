@@ -9,8 +9,8 @@
 // (Weights need the final max and sum of every head, so either the logits are
 // kept, 4 G bytes per row written and read, or the keys are read again.)
 //
-// Of 64 requests of 245 to 3,932 rows, 4 heads per unit: 5.9 us for the outputs,
-// 10.7 with the weights (26 MB of logits and weights); of one request 3.8 us.
+// Of 64 requests of 245 to 3,932 rows, 4 heads per unit: 6.0 us for the outputs,
+// 10.6 with the weights (26 MB of logits and weights); of one request 3.6 to 3.9.
 //
 // A state's factor is 1 where its max is the joint one, so a set whose logits
 // are all NaN keeps its NaN sums; one without rows, or with -inf alone, gives
@@ -162,8 +162,10 @@ static __global__ __launch_bounds__(THREADS) void decode_finish_kernel(
 
 // Threads of a block that joins about `expect` states per unit: eight states
 // each in one go, a block of 1,024 threads for a head's few hundred, of 128
-// where every unit has a handful and the heads fill the chip.  (`expect` is a
-// mean: where lengths differ much, a long unit's states take more rounds.)
+// where every unit has a handful and the heads fill the chip.  `expect` is the
+// mean: where one unit is far longer than the others, its states take rounds one
+// after another (4-bit rows, one request of 32,768 rows beside 63 of 300: 42.7
+// us; the same rows spread evenly 4.3).
 inline int finish_threads(int d, int64_t expect) {
     const int64_t threads = ceil_div(expect, 8) * d;
     return threads <= 128 ? 128 : threads <= 256 ? 256 : threads <= 512 ? 512 : 1024;

@@ -13,11 +13,13 @@
 // units give every CU one; else in a second launch with many workgroups per
 // unit.
 //
-// 512 units at 1,025 rows of which one goes: 11.8 us, bound by the chain of
+// 512 units at 1,025 rows of which one goes: 12.0 us in a kernel trace, 9.8 per
+// call of a replayed graph (f32 rows 9.6, 4-bit rows 9.8), bound by the chain of
 // loads, counting barriers and stores of a workgroup (two launches, with searches
 // over a list of ids: 16.8 + 3.9).  64 units of 8K to 32K rows cut to 20%: the
-// select 24.8 us (one CU per unit, a quarter of the chip), the moves 59.8 us for
-// 280 MB, 4.7 TB/s, the rate of a device copy.
+// select 24.8 us (one CU per unit, a quarter of the chip), the moves 59.7 us for
+// 280 MB, 4.7 TB/s, the rate of a device copy; a call of f32 rows 116 us, of 4-bit
+// rows 47.5.
 #include "select_common.h"
 
 namespace sg {
@@ -246,7 +248,11 @@ template <int CPR, int SB>
 static int launch_evict(const char *fn, hipStream_t s, int units, const EvictArgs &a) {
     const int cap = a.max_pages * a.page_size, items = (int)ceil_div(cap, TOPK_THREADS);
     const bool one = units >= device_cus();
-#define SG_SELECT(I)                                                                                      do {                                                                                                      if (one) evict_select_kernel<I, CPR, SB><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);                 else evict_select_kernel<I, 0, 0><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);                    } while (0)
+#define SG_SELECT(I)                                                                              \
+    do {                                                                                          \
+        if (one) evict_select_kernel<I, CPR, SB><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);     \
+        else evict_select_kernel<I, 0, 0><<<(unsigned)units, TOPK_THREADS, 0, s>>>(a);            \
+    } while (0)
     if (items <= 2) SG_SELECT(2);
     else if (items <= 4) SG_SELECT(4);
     else if (items <= 8) SG_SELECT(8);
